@@ -443,6 +443,114 @@ int lc_update_from_grad(lc_handle* h);
  * synchronous case tau = 1 (Sec. 2, special case): one pass over X, V and G. */
 int lc_update_from_grad_and_average(lc_handle* h);
 
+/* ---- Operators for models whose gradients the caller forms -----------------------------------
+ * Pieces of larger models on the stack of replicas, on arrays that the caller owns: layer
+ * normalisation, the softmax cross-entropy of a last layer with many classes, and the update that
+ * takes an orthogonalised momentum.  Their gradients can be written into the rows that
+ * lc_set_grad() takes (fp32 [m, lc_row_stride(P)]), their parameters read from the rows of X.
+ * None needs a handle, allocates, or synchronises: the work is queued on `stream`, of the device
+ * that is current, and may be captured into a graph.  Calls that overlap need a workspace each.
+ * What a call reads or writes is all it touches: columns behind the last and rows behind the last stay
+ * as they are.  Every result is formed in the same order each time: equal inputs, equal bits. */
+
+/* A matrix per replica in device memory: element (i, r, c) of replica i at p[i * replica + r * row + c];
+ * distances in elements.  Read-only ones may share one matrix between the replicas (replica = 0). */
+typedef struct {
+    void* p;
+    int64_t row;
+    int64_t replica;
+} lc_rows;
+
+/* Layer normalisation of the last axis: y = (x - mean) * r * gain + bias, r = 1 / sqrt(var + eps), mean
+ * and variance (divided by cols) of each row in fp32 whatever the type.
+ *   dtype      : lc_gemm_dtype of x and y (fp32 or bfloat16).  y may stand where x does.
+ *   gain, bias : device fp32 [cols] per replica, param_replica floats apart; NULL: ones, zeros.
+ *   stats      : device fp32 [m, rows, 2], receives mean and r for the backward pass, or NULL.
+ * rows = 0 does nothing.  Errors: LC_ERR_ARG, LC_ERR_ALIGN (a pointer that is not aligned to its
+ * elements), LC_ERR_HIP. */
+int lc_layer_norm(int m, int64_t rows, int32_t cols, int dtype, lc_rows x, const float* gain, const float* bias,
+                  int64_t param_replica, float eps, lc_rows y, float* stats, void* stream);
+
+/* Its backward pass from x, dy and stats: dx (which may stand where x or dy does, not where neither
+ * of them but part of one does), and the sums over the rows dgain = sum dy * (x - mean) * r and dbias =
+ * sum dy, device fp32 [cols] per replica, grad_replica floats apart; NULL: not formed.  They are
+ * written, not added to; rows = 0 gives zeros.  The workspace (device, 256-byte aligned) is needed for
+ * the sums only.  Errors: as above, LC_ERR_WORKSPACE. */
+size_t lc_layer_norm_workspace_bytes(int m, int64_t rows, int32_t cols);
+int lc_layer_norm_grad(int m, int64_t rows, int32_t cols, int dtype, lc_rows x, lc_rows dy, const float* gain,
+                       int64_t param_replica, const float* stats, lc_rows dx, float* dgain, float* dbias,
+                       int64_t grad_replica, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Softmax cross-entropy of a linear last layer, Z = A W + bias, without keeping Z: the loss is the mean
+ * over the rows that count, as lc_loss() and the local steps have it for the last layer of an MLP, for any
+ * number of classes.  A row whose label is not in [0, classes) is left out: its loss is 0, its row of dA
+ * zero, and nothing of its activations gets anywhere.  No row left: loss 0, gradients zero.  A bias of
+ * -infinity takes a class out; a row whose label is such a class has loss +infinity. */
+#define LC_HEAD_MAX_ROWS (1 << 24)
+#define LC_HEAD_MAX_INPUTS (1 << 20)
+#define LC_HEAD_MAX_CLASSES (1 << 22)
+typedef struct {
+    int32_t m;
+    int32_t inputs;
+    int64_t rows;               /* of A, per replica */
+    int32_t classes;
+    int32_t dtype;              /* lc_gemm_dtype of A, W and dA.  fp32: products as accurate as fp32 sums, a
+                                 * factor that is not finite makes the logits it enters NaN.  bfloat16: dZ is rounded
+                                 * to bfloat16 before the two gradient products. */
+    int32_t grad_dtype;         /* of dW and db */
+    lc_rows A;                  /* [rows, inputs] */
+    lc_rows W;                  /* [inputs, classes], as in a row of X.  Its rows are read in place if bfloat16,
+                                 * 16-byte aligned and a multiple of 8 classes; otherwise copied first */
+    const float* bias;          /* fp32 [classes] per replica, or NULL */
+    int64_t bias_replica;
+    const int32_t* labels;      /* device int32 [rows] per replica */
+    int64_t label_replica;
+    float* loss;                /* device fp32 [m] */
+    float* row_loss;            /* device fp32 [rows] per replica, or NULL */
+    int64_t row_loss_replica;
+    /* gradients of loss; read by lc_softmax_head_grad() only */
+    lc_rows dA;                 /* [rows, inputs] */
+    lc_rows dW;                 /* [inputs, classes] */
+    void* db;                   /* [classes] per replica, or NULL */
+    int64_t db_replica;
+} lc_head_args;
+
+/* Bytes of workspace that the call with these arguments needs; 0 if they are refused.  Rows are taken
+ * in chunks so that what is kept for a chunk stays near 2 GB. */
+size_t lc_softmax_head_workspace_bytes(const lc_head_args* args, int with_grad);
+/* loss (and row_loss); and loss with dA, dW and db.  Outputs are written, not added to, and overlap no
+ * input.  Errors: LC_ERR_ARG, LC_ERR_ALIGN (elements; workspace 256 bytes), LC_ERR_UNSUPPORTED (beyond the sizes
+ * above), LC_ERR_WORKSPACE, LC_ERR_HIP. */
+int lc_softmax_head_loss(const lc_head_args* args, void* workspace, size_t workspace_bytes, void* stream);
+int lc_softmax_head_grad(const lc_head_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Orthogonalised direction of a matrix by Newton-Schulz products: from X = src / |src|_F (Frobenius
+ * norm), `steps` (1..16) times X <- 3.4445 X - 4.7750 X X^T X + 2.0315 (X X^T)^2 X.  Singular vectors stay, singular
+ * values go to about 1.  A zero matrix gives zeros; one with an element that is not finite gives NaN.
+ * dst may stand where src does.  dtype: lc_gemm_dtype of both; fp32 results are those of fp32 products.
+ * rows, cols <= LC_ORTHOGONAL_MAX_SIDE.
+ * Errors: LC_ERR_ARG, LC_ERR_ALIGN, LC_ERR_WORKSPACE, LC_ERR_HIP. */
+#define LC_ORTHOGONAL_MAX_SIDE 32768
+size_t lc_orthogonal_workspace_bytes(int m, int32_t rows, int32_t cols, int dtype);
+int lc_orthogonalize(int m, int32_t rows, int32_t cols, int dtype, lc_rows src, lc_rows dst, int steps, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/* One step of a weight matrix [rows = inputs, cols = outputs] of every replica along its orthogonalised
+ * momentum, fp32: v <- beta v + G;  x <- x - lr (s O(v) + wd x), O as above, s = sqrt(max(1, cols / rows)).
+ * With beta = 0, v is not read.  X, V and G are different arrays; the workspace is that of
+ * lc_orthogonal_workspace_bytes(m, rows, cols, LC_GEMM_FP32).  Errors: as above; LC_ERR_ARG for
+ * lr <= 0, beta outside [0, 1) or wd < 0. */
+int lc_update_orthogonal(int m, int32_t rows, int32_t cols, lc_rows X, lc_rows V, lc_rows G, float lr, float beta, float wd,
+                         int steps, void* workspace, size_t workspace_bytes, void* stream);
+
+/* lc_update_from_grad() with that step for every weight matrix of an LC_KIND_MLP run, rate, momentum and decay those of
+ * the handle; biases take the step of lc_update_from_grad().  The iteration counter is unchanged.
+ * workspace: device, 256-byte aligned, lc_update_orthogonal_bytes() bytes (0: not such a run).  Asynchronous.
+ * Errors: LC_ERR_ARG, LC_ERR_STATE (not attached, no gradient set), LC_ERR_UNSUPPORTED (LC_KIND_QUAD),
+ * LC_ERR_ALIGN, LC_ERR_WORKSPACE, LC_ERR_HIP. */
+size_t lc_update_orthogonal_bytes(const lc_handle* h);
+int lc_update_from_grad_orthogonal(lc_handle* h, int steps, void* workspace, size_t workspace_bytes);
+
 /* State access for tests and checkpoints.  X_host / V_host are host fp32 [m, P]
  * (dense, no row padding); either may be NULL.  Both calls synchronise. */
 int lc_get_state(lc_handle* h, float* X_host, float* V_host, int64_t* k);

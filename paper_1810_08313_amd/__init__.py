@@ -13,8 +13,12 @@ from .binding import (  # noqa: F401
     LocalSGD,
     adacomm_next_tau,
     adacomm_next_tau_ex, average_block_momentum_static, STATIC_MAX_PARAMS,
+    layer_norm, layer_norm_grad,
     lc_param_count,
     lc_row_stride,
     lib,
     make_model,
+    orthogonalize,
+    softmax_head_grad, softmax_head_loss,
+    update_orthogonal,
 )

@@ -40,6 +40,35 @@ class LcModel(C.Structure):
     ]
 
 
+class LcRows(C.Structure):
+    """A matrix per replica in device memory, distances in elements."""
+    _fields_ = [("p", C.c_void_p), ("row", C.c_int64), ("replica", C.c_int64)]
+
+
+class LcHeadArgs(C.Structure):
+    _fields_ = [
+        ("m", C.c_int32),
+        ("inputs", C.c_int32),
+        ("rows", C.c_int64),
+        ("classes", C.c_int32),
+        ("dtype", C.c_int32),
+        ("grad_dtype", C.c_int32),
+        ("A", LcRows),
+        ("W", LcRows),
+        ("bias", C.c_void_p),
+        ("bias_replica", C.c_int64),
+        ("labels", C.c_void_p),
+        ("label_replica", C.c_int64),
+        ("loss", C.c_void_p),
+        ("row_loss", C.c_void_p),
+        ("row_loss_replica", C.c_int64),
+        ("dA", LcRows),
+        ("dW", LcRows),
+        ("db", C.c_void_p),
+        ("db_replica", C.c_int64),
+    ]
+
+
 class LcError(RuntimeError):
     def __init__(self, status: int, where: str, hip: int = 0):
         self.status = status
@@ -151,6 +180,30 @@ def lib() -> C.CDLL:
     L.lc_timing_select.argtypes = [vp, C.c_int, C.c_int]
     L.lc_timing_read.restype = C.c_int
     L.lc_timing_read.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_double)]
+    i32, i64, f32, sz = C.c_int32, C.c_int64, C.c_float, C.c_size_t
+    L.lc_layer_norm.restype = C.c_int
+    L.lc_layer_norm.argtypes = [C.c_int, i64, i32, C.c_int, LcRows, vp, vp, i64, f32, LcRows, vp, vp]
+    L.lc_layer_norm_workspace_bytes.restype = sz
+    L.lc_layer_norm_workspace_bytes.argtypes = [C.c_int, i64, i32]
+    L.lc_layer_norm_grad.restype = C.c_int
+    L.lc_layer_norm_grad.argtypes = [C.c_int, i64, i32, C.c_int, LcRows, LcRows, vp, i64, vp, LcRows, vp, vp, i64, vp, sz, vp]
+    hp = C.POINTER(LcHeadArgs)
+    L.lc_softmax_head_workspace_bytes.restype = sz
+    L.lc_softmax_head_workspace_bytes.argtypes = [hp, C.c_int]
+    L.lc_softmax_head_loss.restype = C.c_int
+    L.lc_softmax_head_loss.argtypes = [hp, vp, sz, vp]
+    L.lc_softmax_head_grad.restype = C.c_int
+    L.lc_softmax_head_grad.argtypes = [hp, vp, sz, vp]
+    L.lc_orthogonal_workspace_bytes.restype = sz
+    L.lc_orthogonal_workspace_bytes.argtypes = [C.c_int, i32, i32, C.c_int]
+    L.lc_orthogonalize.restype = C.c_int
+    L.lc_orthogonalize.argtypes = [C.c_int, i32, i32, C.c_int, LcRows, LcRows, C.c_int, vp, sz, vp]
+    L.lc_update_orthogonal.restype = C.c_int
+    L.lc_update_orthogonal.argtypes = [C.c_int, i32, i32, LcRows, LcRows, LcRows, f32, f32, f32, C.c_int, vp, sz, vp]
+    L.lc_update_orthogonal_bytes.restype = sz
+    L.lc_update_orthogonal_bytes.argtypes = [vp]
+    L.lc_update_from_grad_orthogonal.restype = C.c_int
+    L.lc_update_from_grad_orthogonal.argtypes = [vp, C.c_int, vp, sz]
     _lib = L
     return L
 
@@ -214,6 +267,199 @@ def adacomm_next_tau_ex(F0: float, Fl: float, tau0: int, tau_prev: int, gamma: f
     return t
 
 
+# ---- operators on torch tensors whose first axis is the replicas
+#
+# Results and workspaces are allocated by torch on the stream that the call runs on (`stream`, or the tensors' device's
+# current one); results may be given instead: `out`, `dx`, ... of the same shape.  The last axis is contiguous, the
+# other two have any distances, so that a layer's place in the rows of X or G will do.
+
+ERR_ARG, ERR_ALIGN = -1, -4
+
+
+def _need(ok: bool, where: str, what: str) -> None:
+    if not ok:
+        e = LcError(ERR_ARG, where)
+        e.args = (f"{where}: {what} ({ERR_ARG})",)
+        raise e
+
+
+class _Call:
+    """The stream, device and element type that a call's tensors share; checks them."""
+
+    def __init__(self, where: str, first, dtypes, stream):
+        import torch
+        self.torch, self.where, self.device = torch, where, first.device
+        _need(first.is_cuda, where, "tensors of a GPU are needed")
+        _need(first.dtype in dtypes, where, f"element type {first.dtype}")
+        self.stream = stream if stream is not None else torch.cuda.current_stream(first.device)
+        _need(self.stream.device == first.device, where, "the stream is another device's")
+
+    def code(self, dtype) -> int:
+        return GEMM_BF16 if dtype == self.torch.bfloat16 else GEMM_FP32
+
+    def check(self, t, name, shape, dtype) -> None:
+        _need(t.device == self.device, self.where, f"{name} is on {t.device}, not on {self.device}")
+        _need(t.dtype == dtype, self.where, f"{name} has element type {t.dtype}, not {dtype}")
+        _need(tuple(t.shape) == tuple(shape), self.where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+        _need(t.numel() == 0 or t.shape[-1] == 1 or t.stride(-1) == 1, self.where, f"{name}: the last axis is not contiguous")
+
+    def rows(self, t, name, shape, dtype) -> LcRows:
+        self.check(t, name, shape, dtype)
+        return LcRows(t.data_ptr(), t.stride(1), t.stride(0))
+
+    def vector(self, t, name, shape, dtype):
+        """(pointer, distance of replicas) of a [m, n] tensor, or of None."""
+        if t is None:
+            return None, 0
+        self.check(t, name, shape, dtype)
+        return t.data_ptr(), t.stride(0)
+
+    def run(self, fn):
+        """fn() on the call's device, what it allocates belonging to the call's stream."""
+        if self.torch.cuda.current_device() == self.device.index and self.torch.cuda.current_stream(self.device) == self.stream:
+            return fn()
+        with self.torch.cuda.device(self.device), self.torch.cuda.stream(self.stream):
+            return fn()
+
+    def workspace(self, n: int):
+        return self.torch.empty(max(int(n), 1), dtype=self.torch.uint8, device=self.device)
+
+    def status(self, rc: int) -> None:
+        if rc != 0:
+            raise LcError(rc, self.where)
+
+
+def _types(torch):
+    return (torch.float32, torch.bfloat16)
+
+
+def layer_norm(x, gain=None, bias=None, eps: float = 1e-5, out=None, stream=None):
+    """lc_layer_norm on x [m, rows, cols] (fp32 or bfloat16), gain and bias fp32 [m, cols] or None.
+    Returns y and the statistics [m, rows, 2] that layer_norm_grad takes."""
+    import torch
+    c = _Call("lc_layer_norm", x, _types(torch), stream)
+    _need(x.dim() == 3, c.where, "x is [m, rows, cols]")
+    m, rows, cols = x.shape
+
+    def go():
+        y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
+        stats = torch.empty((m, rows, 2), dtype=torch.float32, device=x.device)
+        (gp, gs), (bp, bs) = c.vector(gain, "gain", (m, cols), torch.float32), c.vector(bias, "bias", (m, cols), torch.float32)
+        _need(gain is None or bias is None or gs == bs, c.where, "gain and bias have different distances between replicas")
+        c.status(lib().lc_layer_norm(m, rows, cols, c.code(x.dtype), c.rows(x, "x", x.shape, x.dtype), gp, bp, gs or bs, eps,
+                                     c.rows(y, "out", x.shape, x.dtype), stats.data_ptr(), c.stream.cuda_stream))
+        return y, stats
+    return c.run(go)
+
+
+def layer_norm_grad(x, dy, gain, stats, dx=None, dgain=None, dbias=None, stream=None):
+    """lc_layer_norm_grad: dx, dgain and dbias (fp32 [m, cols]) from dy and what layer_norm returned."""
+    import torch
+    c = _Call("lc_layer_norm_grad", x, _types(torch), stream)
+    _need(x.dim() == 3, c.where, "x is [m, rows, cols]")
+    m, rows, cols = x.shape
+
+    def go():
+        f32 = torch.float32
+        to = torch.empty_like(x, memory_format=torch.contiguous_format) if dx is None else dx
+        dg = torch.empty((m, cols), dtype=f32, device=x.device) if dgain is None else dgain
+        db = torch.empty((m, cols), dtype=f32, device=x.device) if dbias is None else dbias
+        c.check(stats, "stats", (m, rows, 2), f32)
+        _need(stats.is_contiguous(), c.where, "stats is not contiguous")
+        gp, gs = c.vector(gain, "gain", (m, cols), f32)
+        (dgp, dgs), (dbp, dbs) = c.vector(dg, "dgain", (m, cols), f32), c.vector(db, "dbias", (m, cols), f32)
+        _need(m == 1 or dgs == dbs, c.where, "dgain and dbias have different distances between replicas")
+        n = lib().lc_layer_norm_workspace_bytes(m, rows, cols)
+        ws = c.workspace(n)
+        c.status(lib().lc_layer_norm_grad(m, rows, cols, c.code(x.dtype), c.rows(x, "x", x.shape, x.dtype),
+                                          c.rows(dy, "dy", x.shape, x.dtype), gp, gs, stats.data_ptr(),
+                                          c.rows(to, "dx", x.shape, x.dtype), dgp, dbp, dgs, ws.data_ptr(), n,
+                                          c.stream.cuda_stream))
+        return to, dg, db
+    return c.run(go)
+
+
+def _softmax_head(where, A, W, bias, labels, grads, stream):
+    import torch
+    c = _Call(where, A, _types(torch), stream)
+    _need(A.dim() == 3 and W.dim() == 3, where, "A is [m, rows, inputs], W [m, inputs, classes]")
+    m, rows, d = A.shape
+    classes = W.shape[2]
+
+    def go():
+        f32 = torch.float32
+        h = LcHeadArgs(m=m, inputs=d, rows=rows, classes=classes, dtype=c.code(A.dtype))
+        h.A, h.W = c.rows(A, "A", A.shape, A.dtype), c.rows(W, "W", (m, d, classes), A.dtype)
+        h.bias, h.bias_replica = c.vector(bias, "bias", (m, classes), f32)
+        h.labels, h.label_replica = c.vector(labels, "labels", (m, rows), torch.int32)
+        loss = torch.empty(m, dtype=f32, device=A.device)
+        row_loss = torch.empty((m, rows), dtype=f32, device=A.device)
+        h.loss, h.row_loss, h.row_loss_replica = loss.data_ptr(), row_loss.data_ptr(), rows
+        if grads is None:
+            n = lib().lc_softmax_head_workspace_bytes(C.byref(h), 0)
+            ws = c.workspace(n)
+            c.status(lib().lc_softmax_head_loss(C.byref(h), ws.data_ptr(), n, c.stream.cuda_stream))
+            return loss, row_loss
+        dA, dW, db, dtype = grads
+        dtype = dtype or (dW.dtype if dW is not None else A.dtype)
+        _need(dtype in _types(torch), where, f"gradients of element type {dtype}")
+        dA = torch.empty((m, rows, d), dtype=A.dtype, device=A.device) if dA is None else dA
+        dW = torch.empty((m, d, classes), dtype=dtype, device=A.device) if dW is None else dW
+        db = torch.empty((m, classes), dtype=dtype, device=A.device) if db is None else db
+        h.grad_dtype = c.code(dtype)
+        h.dA, h.dW = c.rows(dA, "dA", A.shape, A.dtype), c.rows(dW, "dW", (m, d, classes), dtype)
+        h.db, h.db_replica = c.vector(db, "db", (m, classes), dtype)
+        n = lib().lc_softmax_head_workspace_bytes(C.byref(h), 1)
+        ws = c.workspace(n)
+        c.status(lib().lc_softmax_head_grad(C.byref(h), ws.data_ptr(), n, c.stream.cuda_stream))
+        return loss, dA, dW, db
+    return c.run(go)
+
+
+def softmax_head_loss(A, W, bias, labels, stream=None):
+    """lc_softmax_head_loss: mean cross-entropy [m] of Z = A W + bias and the rows' [m, rows]; A [m, rows, inputs] and
+    W [m, inputs, classes] fp32 or bfloat16, bias fp32 [m, classes] or None, labels int32 [m, rows]."""
+    return _softmax_head("lc_softmax_head_loss", A, W, bias, labels, None, stream)
+
+
+def softmax_head_grad(A, W, bias, labels, dA=None, dW=None, db=None, grad_dtype=None, stream=None):
+    """lc_softmax_head_grad: the loss [m], dA, dW and db (the last two of grad_dtype, A's element type by default)."""
+    return _softmax_head("lc_softmax_head_grad", A, W, bias, labels, (dA, dW, db, grad_dtype), stream)
+
+
+def orthogonalize(src, steps: int = 5, out=None, stream=None):
+    """lc_orthogonalize of src [m, rows, cols], fp32 or bfloat16."""
+    import torch
+    c = _Call("lc_orthogonalize", src, _types(torch), stream)
+    _need(src.dim() == 3, c.where, "src is [m, rows, cols]")
+    m, rows, cols = src.shape
+
+    def go():
+        to = torch.empty_like(src, memory_format=torch.contiguous_format) if out is None else out
+        n = lib().lc_orthogonal_workspace_bytes(m, rows, cols, c.code(src.dtype))
+        ws = c.workspace(n)
+        c.status(lib().lc_orthogonalize(m, rows, cols, c.code(src.dtype), c.rows(src, "src", src.shape, src.dtype),
+                                        c.rows(to, "out", src.shape, src.dtype), int(steps), ws.data_ptr(), n,
+                                        c.stream.cuda_stream))
+        return to
+    return c.run(go)
+
+
+def update_orthogonal(X, V, G, lr: float, beta: float, wd: float = 0.0, steps: int = 5, stream=None) -> None:
+    """lc_update_orthogonal of X and V in place, fp32 [m, rows, cols] each."""
+    import torch
+    c = _Call("lc_update_orthogonal", X, (torch.float32,), stream)
+    _need(X.dim() == 3, c.where, "X is [m, rows, cols]")
+    m, rows, cols = X.shape
+
+    def go():
+        n = lib().lc_orthogonal_workspace_bytes(m, rows, cols, GEMM_FP32)
+        ws = c.workspace(n)
+        c.status(lib().lc_update_orthogonal(m, rows, cols, *(c.rows(t, k, X.shape, X.dtype) for t, k in ((X, "X"), (V, "V"), (G, "G"))),
+                                            lr, beta, wd, int(steps), ws.data_ptr(), n, c.stream.cuda_stream))
+    c.run(go)
+
+
 class LocalSGD:
     """One m-replica run on the current CUDA/HIP device.
 
@@ -241,7 +487,7 @@ class LocalSGD:
         self._h = h
         self.X = torch.zeros((self.m, self.Ps), dtype=torch.float32, device=self.device)
         self.V = torch.zeros((self.m, self.Ps), dtype=torch.float32, device=self.device)
-        self.G = None
+        self.G = self.orth_scratch = None
         ws = int(self._L.lc_workspace_bytes(self._h))
         self.scratch = torch.empty(ws, dtype=torch.uint8, device=self.device)
         self.data = self.labels = self.qa = self.qc = None
@@ -416,6 +662,15 @@ class LocalSGD:
 
     def update_from_grad(self) -> None:
         self._check(self._L.lc_update_from_grad(self._h), "lc_update_from_grad")
+
+    def update_from_grad_orthogonal(self, steps: int = 5) -> None:
+        """The update from the gradients of set_grad() with every weight matrix' momentum orthogonalised."""
+        n = int(self._L.lc_update_orthogonal_bytes(self._h))
+        if self.orth_scratch is None and n:
+            with self._torch.cuda.stream(self.stream):
+                self.orth_scratch = self._torch.empty(n, dtype=self._torch.uint8, device=self.device)
+        self._check(self._L.lc_update_from_grad_orthogonal(self._h, int(steps), self.orth_scratch.data_ptr() if n else None, n),
+                    "lc_update_from_grad_orthogonal")
 
     def update_from_grad_and_average(self) -> None:
         self._check(self._L.lc_update_from_grad_and_average(self._h), "lc_update_from_grad_and_average")

@@ -1,0 +1,429 @@
+// Layer normalisation of the last axis and its backward pass, a gain and a bias per replica.
+//
+//   n = (x - mean) r,  r = 1 / sqrt(var + eps),  y = n gain + bias
+//   h = dy gain;  dx = r (h - mean(h) - n mean(h n));  dgain = sum_rows dy n;  dbias = sum_rows dy
+//
+// Memory-bound: 8 to 14 operations a value against 4 to 12 bytes.  A row stays in registers between its
+// passes (mean, then squares of differences: no cancellation at large offsets), so that every array crosses
+// memory once.  A row belongs to a wavefront (up to 512 columns) or to a workgroup; each thread keeps
+// its columns for all rows that its workgroup takes, so that the sums over rows stay in registers too and
+// leave as one partial row per workgroup, added up in a fixed order by a second kernel: no atomics, the
+// same result every time.  Rows wider than the registers hold are read again instead.
+#include "lc_operators.h"
+
+namespace lc {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kMaxHeld = 32;   // values of a row that a thread of the forward kernel holds
+
+struct NormArgs {
+    const void *x, *dy;
+    void* y;                     // forward: y, backward: dx
+    const float *gain, *bias;
+    float* stats;                // forward: written (may be null), backward: read
+    int64_t x_row, x_rep, dy_row, dy_rep, y_row, y_rep, param_rep;
+    float* partial;              // [m][blocks][2][cols]
+    int64_t rows;
+    int cols, blocks;            // workgroups of a replica
+    float eps, inv_cols;
+};
+
+template <typename T, int W>
+struct Chunk;
+template <>
+struct Chunk<float, 1> {
+    float v[1];
+    __device__ __forceinline__ void load(const float* p) { v[0] = *p; }
+    __device__ __forceinline__ void store(float* p) const { *p = v[0]; }
+};
+template <>
+struct Chunk<bf16_t, 1> {
+    float v[1];
+    __device__ __forceinline__ void load(const bf16_t* p) { v[0] = static_cast<float>(*p); }
+    __device__ __forceinline__ void store(bf16_t* p) const { *p = static_cast<bf16_t>(v[0]); }
+};
+template <>
+struct Chunk<float, 4> {
+    float v[4];
+    __device__ __forceinline__ void load(const float* p) {
+        const f32x4 t = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = t[e];
+    }
+    __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]}; }
+};
+template <>
+struct Chunk<bf16_t, 8> {
+    float v[8];
+    __device__ __forceinline__ void load(const bf16_t* p) {
+        const bf16x8 t = *reinterpret_cast<const bf16x8*>(p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(t[e]);
+    }
+    __device__ __forceinline__ void store(bf16_t* p) const {
+        bf16x8 t;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = static_cast<bf16_t>(v[e]);
+        *reinterpret_cast<bf16x8*>(p) = t;
+    }
+};
+
+// Sums of N values over the threads that share a row: a wavefront, or the workgroup through LDS (the two
+// halves of `lds` in turn, so that one barrier is enough).
+template <int GROUP, int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], float* lds, int& turn) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+    if constexpr (GROUP > 64) {
+        float* to = lds + turn * 16;
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) to[(threadIdx.x >> 6) * 2 + i] = s[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s[i] = (to[i] + to[2 + i]) + (to[4 + i] + to[6 + i]);
+            if constexpr (GROUP > 256) s[i] += (to[8 + i] + to[10 + i]) + (to[12 + i] + to[14 + i]);
+        }
+    }
+}
+
+// H chunks of W values per thread cover a row; GROUP threads share it.
+template <typename T, int GROUP, int W, int H>
+__global__ void __launch_bounds__(kBlock) norm_kernel(NormArgs a) {
+    __shared__ float lds[32];
+    const int t = threadIdx.x % GROUP, i = blockIdx.y;
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * (kBlock / GROUP) + threadIdx.x / GROUP; row < a.rows;
+         row += (int64_t)gridDim.x * (kBlock / GROUP)) {
+        const T* x = static_cast<const T*>(a.x) + i * a.x_rep + row * a.x_row;
+        T* y = static_cast<T*>(a.y) + i * a.y_rep + row * a.y_row;
+        Chunk<T, W> v[H];
+        float s[1] = {0.f};
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            const int c = (h * GROUP + t) * W;
+            if (c < a.cols) v[h].load(x + c);
+        }
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+            if ((h * GROUP + t) * W < a.cols)
+#pragma unroll
+                for (int e = 0; e < W; ++e) s[0] += v[h].v[e];
+        row_sums<GROUP>(s, lds, turn);
+        const float mean = s[0] * a.inv_cols;
+        s[0] = 0.f;
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+            if ((h * GROUP + t) * W < a.cols)
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    v[h].v[e] -= mean;
+                    s[0] += v[h].v[e] * v[h].v[e];
+                }
+        row_sums<GROUP>(s, lds, turn);
+        const float r = 1.f / sqrtf(s[0] * a.inv_cols + a.eps);
+        if (a.stats && t == 0) {
+            float* st = a.stats + ((int64_t)i * a.rows + row) * 2;
+            st[0] = mean;
+            st[1] = r;
+        }
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            const int c = (h * GROUP + t) * W;
+            if (c >= a.cols) continue;
+            Chunk<T, W> o;
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                o.v[e] = v[h].v[e] * r;
+                if (a.gain) o.v[e] *= a.gain[i * a.param_rep + c + e];
+                if (a.bias) o.v[e] += a.bias[i * a.param_rep + c + e];
+            }
+            o.store(y + c);
+        }
+    }
+}
+
+// Rows that do not fit: read three times, from the caches as a rule.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) norm_wide_kernel(NormArgs a) {
+    __shared__ float lds[32];
+    const int i = blockIdx.y;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T* x = static_cast<const T*>(a.x) + i * a.x_rep + row * a.x_row;
+        T* y = static_cast<T*>(a.y) + i * a.y_rep + row * a.y_row;
+        float s[1] = {0.f};
+        for (int c = threadIdx.x; c < a.cols; c += kBlock) s[0] += static_cast<float>(x[c]);
+        row_sums<kBlock>(s, lds, turn);
+        const float mean = s[0] * a.inv_cols;
+        s[0] = 0.f;
+        for (int c = threadIdx.x; c < a.cols; c += kBlock) {
+            const float d = static_cast<float>(x[c]) - mean;
+            s[0] += d * d;
+        }
+        row_sums<kBlock>(s, lds, turn);
+        const float r = 1.f / sqrtf(s[0] * a.inv_cols + a.eps);
+        if (a.stats && threadIdx.x == 0) {
+            float* st = a.stats + ((int64_t)i * a.rows + row) * 2;
+            st[0] = mean;
+            st[1] = r;
+        }
+        for (int c = threadIdx.x; c < a.cols; c += kBlock) {
+            float o = (static_cast<float>(x[c]) - mean) * r;
+            if (a.gain) o *= a.gain[i * a.param_rep + c];
+            if (a.bias) o += a.bias[i * a.param_rep + c];
+            y[c] = static_cast<T>(o);
+        }
+    }
+}
+
+template <typename T, int GROUP, int W, int H>
+__global__ void __launch_bounds__(GROUP > kBlock ? GROUP : kBlock) norm_grad_kernel(NormArgs a) {
+    constexpr int kGroups = GROUP > kBlock ? 1 : kBlock / GROUP;
+    __shared__ float lds[32];
+    __shared__ float sums[kGroups > 1 ? kGroups * 2 * GROUP * W * H : 1];
+    const int t = threadIdx.x % GROUP, group = threadIdx.x / GROUP, i = blockIdx.y;
+    int turn = 0;
+    float gain[H * W], dg[H * W], db[H * W];
+#pragma unroll
+    for (int k = 0; k < H * W; ++k) {
+        const int c = (k / W * GROUP + t) * W + k % W;
+        gain[k] = a.gain && c < a.cols ? a.gain[i * a.param_rep + c] : 1.f;
+        dg[k] = db[k] = 0.f;
+    }
+    for (int64_t row = (int64_t)blockIdx.x * kGroups + group; row < a.rows; row += (int64_t)gridDim.x * kGroups) {
+        const T* x = static_cast<const T*>(a.x) + i * a.x_rep + row * a.x_row;
+        const T* dy = static_cast<const T*>(a.dy) + i * a.dy_rep + row * a.dy_row;
+        T* dx = static_cast<T*>(a.y) + i * a.y_rep + row * a.y_row;
+        Chunk<T, W> n[H], h[H];
+        const float* st = a.stats + ((int64_t)i * a.rows + row) * 2;
+        const float mean = st[0], r = st[1];
+#pragma unroll
+        for (int k = 0; k < H; ++k) {
+            const int c = (k * GROUP + t) * W;
+            if (c < a.cols) {
+                n[k].load(x + c);
+                h[k].load(dy + c);
+            }
+        }
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < H; ++k)
+            if ((k * GROUP + t) * W < a.cols)
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    n[k].v[e] = (n[k].v[e] - mean) * r;
+                    dg[k * W + e] += h[k].v[e] * n[k].v[e];
+                    db[k * W + e] += h[k].v[e];
+                    h[k].v[e] *= gain[k * W + e];
+                    s[0] += h[k].v[e];
+                    s[1] += h[k].v[e] * n[k].v[e];
+                }
+        row_sums<GROUP>(s, lds, turn);
+        const float c1 = s[0] * a.inv_cols, c2 = s[1] * a.inv_cols;
+#pragma unroll
+        for (int k = 0; k < H; ++k) {
+            const int c = (k * GROUP + t) * W;
+            if (c >= a.cols) continue;
+            Chunk<T, W> o;
+#pragma unroll
+            for (int e = 0; e < W; ++e) o.v[e] = r * (h[k].v[e] - c1 - n[k].v[e] * c2);
+            o.store(dx + c);
+        }
+    }
+    if (!a.partial) return;
+    float* out = a.partial + ((int64_t)i * a.blocks + blockIdx.x) * 2 * a.cols;
+    if constexpr (kGroups > 1) {
+#pragma unroll
+        for (int k = 0; k < H * W; ++k) {
+            const int c = (k / W * GROUP + t) * W + k % W;
+            sums[group * 2 * GROUP * W * H + c] = dg[k];
+            sums[(group * 2 + 1) * GROUP * W * H + c] = db[k];
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.cols; c += kBlock) {
+            float g = 0.f, b = 0.f;
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j) {
+                g += sums[j * 2 * GROUP * W * H + c];
+                b += sums[(j * 2 + 1) * GROUP * W * H + c];
+            }
+            out[c] = g;
+            out[a.cols + c] = b;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < H * W; ++k) {
+            const int c = (k / W * GROUP + t) * W + k % W;
+            if (c < a.cols) {
+                out[c] = dg[k];
+                out[a.cols + c] = db[k];
+            }
+        }
+    }
+}
+
+// Rows that do not fit: dx here, the sums over rows in norm_columns_kernel.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) norm_grad_wide_kernel(NormArgs a) {
+    __shared__ float lds[32];
+    const int i = blockIdx.y;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T* x = static_cast<const T*>(a.x) + i * a.x_rep + row * a.x_row;
+        const T* dy = static_cast<const T*>(a.dy) + i * a.dy_rep + row * a.dy_row;
+        T* dx = static_cast<T*>(a.y) + i * a.y_rep + row * a.y_row;
+        const float* st = a.stats + ((int64_t)i * a.rows + row) * 2;
+        const float mean = st[0], r = st[1];
+        float s[2] = {0.f, 0.f};
+        for (int c = threadIdx.x; c < a.cols; c += kBlock) {
+            const float h = static_cast<float>(dy[c]) * (a.gain ? a.gain[i * a.param_rep + c] : 1.f);
+            s[0] += h;
+            s[1] += h * (static_cast<float>(x[c]) - mean) * r;
+        }
+        row_sums<kBlock>(s, lds, turn);
+        const float c1 = s[0] * a.inv_cols, c2 = s[1] * a.inv_cols;
+        for (int c = threadIdx.x; c < a.cols; c += kBlock) {
+            const float h = static_cast<float>(dy[c]) * (a.gain ? a.gain[i * a.param_rep + c] : 1.f);
+            dx[c] = static_cast<T>(r * (h - c1 - (static_cast<float>(x[c]) - mean) * r * c2));
+        }
+    }
+}
+template <typename T>
+__global__ void __launch_bounds__(kBlock) norm_columns_kernel(NormArgs a) {
+    const int i = blockIdx.z, c = blockIdx.y * kBlock + threadIdx.x;
+    if (c >= a.cols) return;
+    float g = 0.f, b = 0.f;
+    for (int64_t row = blockIdx.x; row < a.rows; row += a.blocks) {
+        const float* st = a.stats + ((int64_t)i * a.rows + row) * 2;
+        const float d = static_cast<float>(static_cast<const T*>(a.dy)[i * a.dy_rep + row * a.dy_row + c]);
+        g += d * (static_cast<float>(static_cast<const T*>(a.x)[i * a.x_rep + row * a.x_row + c]) - st[0]) * st[1];
+        b += d;
+    }
+    float* out = a.partial + ((int64_t)i * a.blocks + blockIdx.x) * 2 * a.cols;
+    out[c] = g;
+    out[a.cols + c] = b;
+}
+
+// The partial rows added up: 64 columns per workgroup, 4 wavefronts each a quarter of the rows.
+__global__ void __launch_bounds__(kBlock) norm_reduce_kernel(const float* partial, int blocks, int cols, float* dgain, float* dbias,
+                                                             int64_t grad_rep) {
+    __shared__ float s[4][64];
+    const int i = blockIdx.y, which = blockIdx.z, w = threadIdx.x >> 6, c = blockIdx.x * 64 + (threadIdx.x & 63);
+    float* out = which ? dbias : dgain;
+    if (!out) return;
+    float v = 0.f;
+    if (c < cols)
+        for (int b = w; b < blocks; b += 4) v += partial[((int64_t)i * blocks + b) * 2 * cols + (int64_t)which * cols + c];
+    s[w][threadIdx.x & 63] = v;
+    __syncthreads();
+    if (w == 0 && c < cols) out[i * grad_rep + c] = (s[0][threadIdx.x] + s[1][threadIdx.x]) + (s[2][threadIdx.x] + s[3][threadIdx.x]);
+}
+
+// Workgroups that a replica's rows are shared out to: the whole chip several times over with all replicas
+// together, but not more than there are rows to take.
+int norm_blocks(int m, int64_t rows, int cols) {
+    const int per = cols <= 512 ? kBlock / 64 : 1;
+    const int64_t want = std::max<int64_t>(1, 1024 / m);
+    return static_cast<int>(std::max<int64_t>(1, std::min(want, (rows + per - 1) / per)));
+}
+
+template <typename T, int W>
+void launch_norm(const NormArgs& a, int m, hipStream_t st) {
+    const int held = (a.cols + 63) / 64;
+    if (held <= 8) {   // a wavefront a row
+        const dim3 g(static_cast<unsigned>(std::min<int64_t>((a.rows + 3) / 4, 1 << 16)), m);
+        norm_kernel<T, 64, W, 8 / W><<<g, kBlock, 0, st>>>(a);
+        return;
+    }
+    const dim3 g(static_cast<unsigned>(std::min<int64_t>(a.rows, 1 << 16)), m);
+    if (a.cols <= kBlock * 8) norm_kernel<T, kBlock, W, 8 / W><<<g, kBlock, 0, st>>>(a);
+    else if (a.cols <= kBlock * 16) norm_kernel<T, kBlock, W, 16 / W><<<g, kBlock, 0, st>>>(a);
+    else if (a.cols <= kBlock * kMaxHeld) norm_kernel<T, kBlock, W, kMaxHeld / W><<<g, kBlock, 0, st>>>(a);
+    else norm_wide_kernel<T><<<g, kBlock, 0, st>>>(a);
+}
+
+template <typename T, int W>
+void launch_norm_grad(const NormArgs& a, int m, hipStream_t st) {
+    const dim3 g(a.blocks, m);
+    if (a.cols <= 512) norm_grad_kernel<T, 64, W, 8 / W><<<g, kBlock, 0, st>>>(a);
+    else if (a.cols <= kBlock * 8) norm_grad_kernel<T, kBlock, W, 8 / W><<<g, kBlock, 0, st>>>(a);
+    else if (a.cols <= kBlock * 16) norm_grad_kernel<T, kBlock, W, 16 / W><<<g, kBlock, 0, st>>>(a);
+    else if (a.cols <= 512 * 16) norm_grad_kernel<T, 512, W, 16 / W><<<g, 512, 0, st>>>(a);
+    else {
+        // the sums first: dx may stand where dy or x does
+        if (a.partial) norm_columns_kernel<T><<<dim3(a.blocks, (a.cols + kBlock - 1) / kBlock, m), kBlock, 0, st>>>(a);
+        norm_grad_wide_kernel<T><<<g, kBlock, 0, st>>>(a);
+    }
+}
+
+// Whether every row of every replica starts where a 16-byte load may.
+bool rows_vector(const lc_rows& r, int m, int64_t rows, size_t e) {
+    return aligned_to(r.p, 16) && (rows <= 1 || r.row * e % 16 == 0) && (m <= 1 || r.replica * e % 16 == 0);
+}
+
+}  // namespace
+}  // namespace lc
+
+using namespace lc;
+
+extern "C" {
+
+int lc_layer_norm(int m, int64_t rows, int32_t cols, int dtype, lc_rows x, const float* gain, const float* bias,
+                  int64_t param_replica, float eps, lc_rows y, float* stats, void* stream) {
+    if (m < 1 || m > kMaxReplicas || rows < 0 || cols < 1 || (dtype != LC_GEMM_FP32 && dtype != LC_GEMM_BF16)) return LC_ERR_ARG;
+    if (!(eps >= 0.f) || param_replica < 0) return LC_ERR_ARG;
+    if (rows == 0) return LC_OK;
+    int rc = check_input(x, m, rows, cols, dtype);
+    if (rc == LC_OK) rc = check_output(y, m, rows, cols, dtype);
+    if (rc != LC_OK) return rc;
+    if (!aligned_to(gain, 4) || !aligned_to(bias, 4) || !aligned_to(stats, 4)) return LC_ERR_ALIGN;
+    const size_t e = element_bytes(dtype);
+    NormArgs a{x.p, nullptr, y.p, gain, bias, stats, x.row, x.replica, 0, 0, y.row, y.replica, param_replica,
+               nullptr, rows, cols, 0, eps, 1.f / static_cast<float>(cols)};
+    const bool vec = rows_vector(x, m, rows, e) && rows_vector(y, m, rows, e) && cols * e % 16 == 0;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (dtype == LC_GEMM_BF16) vec ? launch_norm<bf16_t, 8>(a, m, st) : launch_norm<bf16_t, 1>(a, m, st);
+    else vec ? launch_norm<float, 4>(a, m, st) : launch_norm<float, 1>(a, m, st);
+    return hipGetLastError() == hipSuccess ? LC_OK : LC_ERR_HIP;
+}
+
+size_t lc_layer_norm_workspace_bytes(int m, int64_t rows, int32_t cols) {
+    if (m < 1 || rows < 1 || cols < 1) return 0;
+    return sizeof(float) * 2 * static_cast<size_t>(cols) * static_cast<size_t>(norm_blocks(m, rows, cols)) * static_cast<size_t>(m);
+}
+
+int lc_layer_norm_grad(int m, int64_t rows, int32_t cols, int dtype, lc_rows x, lc_rows dy, const float* gain,
+                       int64_t param_replica, const float* stats, lc_rows dx, float* dgain, float* dbias,
+                       int64_t grad_replica, void* workspace, size_t workspace_bytes, void* stream) {
+    if (m < 1 || m > kMaxReplicas || rows < 0 || cols < 1 || (dtype != LC_GEMM_FP32 && dtype != LC_GEMM_BF16)) return LC_ERR_ARG;
+    if (param_replica < 0 || ((dgain || dbias) && m > 1 && grad_replica < cols)) return LC_ERR_ARG;
+    if (!aligned_to(gain, 4) || !aligned_to(stats, 4) || !aligned_to(dgain, 4) || !aligned_to(dbias, 4)) return LC_ERR_ALIGN;
+    if (rows > 0) {
+        int rc = check_input(x, m, rows, cols, dtype);
+        if (rc == LC_OK) rc = check_input(dy, m, rows, cols, dtype);
+        if (rc == LC_OK) rc = check_output(dx, m, rows, cols, dtype);
+        if (rc != LC_OK) return rc;
+        if (!stats) return LC_ERR_ARG;
+    }
+    const bool sums = dgain || dbias;
+    if (sums && rows > 0 && (!workspace || workspace_bytes < lc_layer_norm_workspace_bytes(m, rows, cols))) return LC_ERR_WORKSPACE;
+    if (sums && !aligned_to(workspace, 256)) return LC_ERR_ALIGN;
+    const size_t e = element_bytes(dtype);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    NormArgs a{x.p, dy.p, dx.p, gain, nullptr, const_cast<float*>(stats), x.row, x.replica, dy.row, dy.replica, dx.row, dx.replica,
+               param_replica, sums ? static_cast<float*>(workspace) : nullptr, rows, cols, rows ? norm_blocks(m, rows, cols) : 0, 0.f,
+               1.f / static_cast<float>(cols)};
+    if (rows > 0) {
+        const bool vec = rows_vector(x, m, rows, e) && rows_vector(dy, m, rows, e) && rows_vector(dx, m, rows, e) && cols * e % 16 == 0;
+        if (dtype == LC_GEMM_BF16) vec ? launch_norm_grad<bf16_t, 8>(a, m, st) : launch_norm_grad<bf16_t, 1>(a, m, st);
+        else vec ? launch_norm_grad<float, 4>(a, m, st) : launch_norm_grad<float, 1>(a, m, st);
+    }
+    if (sums) norm_reduce_kernel<<<dim3((cols + 63) / 64, m, 2), kBlock, 0, st>>>(a.partial, a.blocks, cols, dgain, dbias, grad_replica);
+    return hipGetLastError() == hipSuccess ? LC_OK : LC_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,55 @@
+// What the operators on caller-owned arrays share (lc_layer_norm, lc_softmax_head, lc_orthogonalize and their
+// gradients): checks of arguments on the host, sums over a wavefront and a workgroup on the device.
+#pragma once
+#include <algorithm>
+
+#include "lc_internal.h"
+
+namespace lc {
+namespace {
+
+constexpr int64_t kMaxReplicas = 65535;
+
+inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+inline size_t element_bytes(int dtype) { return dtype == LC_GEMM_BF16 ? 2 : 4; }
+
+// A matrix per replica that is read: rows may be shared between replicas (replica = 0).
+inline int check_input(const lc_rows& a, int m, int64_t rows, int64_t cols, int dtype) {
+    if (!a.p || a.replica < 0 || (rows > 1 && a.row < cols)) return LC_ERR_ARG;
+    (void)m;
+    return aligned_to(a.p, element_bytes(dtype)) ? LC_OK : LC_ERR_ALIGN;
+}
+// ... that is written: no element has two places.
+inline int check_output(const lc_rows& a, int m, int64_t rows, int64_t cols, int dtype) {
+    const int rc = check_input(a, m, rows, cols, dtype);
+    if (rc != LC_OK) return rc;
+    const int64_t r = rows > 1 ? a.row : cols;
+    const bool apart = m == 1 || a.replica >= (rows - 1) * r + cols || (rows > 1 && r >= (m - 1) * a.replica + cols && a.replica >= cols);
+    return apart ? LC_OK : LC_ERR_ARG;
+}
+
+// Hands out parts of a workspace; with a null base it only counts.
+struct Carver {
+    char* base;
+    size_t used = 0;
+    template <typename T>
+    T* take(int64_t n) {
+        T* p = base ? reinterpret_cast<T*>(base + used) : nullptr;
+        used += (static_cast<size_t>(std::max<int64_t>(n, 0)) * sizeof(T) + 255) & ~static_cast<size_t>(255);
+        return p;
+    }
+};
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+
+}  // namespace
+}  // namespace lc

@@ -1,0 +1,739 @@
+// Softmax cross-entropy over many classes behind a linear layer, and its gradient, per replica:
+//
+//   Z = A W + b,  loss = mean over kept rows of (log sum_c exp z_c - z_y)
+//   dZ = softmax(Z) - onehot(y),  dA = dZ W^T / kept,  dW = A^T dZ / kept,  db = sum_rows dZ / kept
+//
+// Bound by three products of rows x inputs x classes where the batch is long, by reading W twice and writing dW
+// once where it is short.  Z itself never reaches memory: the product's workgroup, 256 classes wide, reduces its
+// part of a row to a maximum and a sum of exponentials, and the parts of a row are joined afterwards.  For the
+// gradient it leaves e = exp(z - the part's maximum), for as many rows at a time as 2 GB hold; with the joined sum a
+// second pass turns e into dZ in place (and sums its columns, db), which the two gradient products read.  Leaving e
+// costs 6 bytes a row and class where forming Z again costs 2 * inputs operations: at 1.0 PFLOP/s and 4.5 TB/s the
+// product is the dearer one from about 700 inputs on.
+//
+// Kept rows are moved together first, in their order: rows whose label is outside the classes cost nothing and
+// nothing of them, an infinity in their activations neither, gets into a sum.
+//
+// bf16 operands: e is kept as fp16 times 2^15 (11 bits down to 2^-29 of the part's maximum), dZ rounded to bf16
+// once and divided by the number of rows behind the sums (so that the label's -1 stays exact: 1 / kept would be off by
+// up to 2^-9 in every row, the same way), sums in 32 bits.  The label's own delta is -(sum of the others) / (whole sum), formed in 32 bits: p - 1 would
+// keep no digits of a well-fitted row.
+// fp32 operands: the exact sum of three bf16 parts each, six of the nine part products (what is left out is below
+// 2^-24 of |a| |b|), e and dZ in 32 bits.
+#include "lc_operators.h"
+#include "lc_tile_product.h"
+
+namespace lc {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kWide = 256;                        // classes of a workgroup of the first product: the parts of a row
+constexpr int64_t kKeepBytes = 2147483648LL;      // of e, and what stands beside it, at a time
+constexpr float kEScale = 32768.f;
+
+__device__ __forceinline__ uint16_t bits(bf16_t x) { return __builtin_bit_cast(uint16_t, x); }
+// x as the sum of three bf16 (24 bits: exact unless the last parts leave the exponent range).
+__device__ __forceinline__ void split3(float x, uint16_t (&p)[3]) {
+    const bf16_t a = static_cast<bf16_t>(x);
+    const float r = x - static_cast<float>(a);
+    const bf16_t b = static_cast<bf16_t>(r);
+    p[0] = bits(a);
+    p[1] = bits(b);
+    p[2] = bits(static_cast<bf16_t>(r - static_cast<float>(b)));
+}
+
+// ------------------------------------------------------------------ kept rows
+
+// order[0 .. kept): rows that count, in their order; behind them the others, whose loss is zero.
+__global__ void __launch_bounds__(1024) head_rows_kernel(const int32_t* labels, int64_t label_rep, int rows, int classes, int32_t* order,
+                                                         int32_t* kept_label, int* kept, float* row_loss, int64_t loss_rep) {
+    __shared__ int part[16];
+    const int i = blockIdx.x, w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    labels += i * label_rep;
+    order += (int64_t)i * rows;
+    kept_label += (int64_t)i * rows;
+    int total = 0;
+    for (int pass = 0; pass < 2; ++pass) {
+        int before = 0;   // kept rows ahead of this round's
+        for (int r0 = 0; r0 < rows; r0 += 1024) {
+            const int r = r0 + threadIdx.x;
+            const int y = r < rows ? labels[r] : -1;
+            const bool keep = y >= 0 && y < classes;
+            const uint64_t mask = __ballot(keep);
+            if (lane == 0) part[w] = __popcll(mask);
+            __syncthreads();
+            int mine = before + __popcll(mask & ((1ULL << lane) - 1));
+            for (int k = 0; k < 16; ++k) {
+                if (k < w) mine += part[k];
+                before += part[k];
+            }
+            if (pass == 1 && r < rows) {
+                const int at = keep ? mine : total + r - mine;
+                order[at] = r;
+                kept_label[at] = keep ? y : -1;
+                if (!keep && row_loss) row_loss[i * loss_rep + r] = 0.f;
+            }
+            __syncthreads();
+        }
+        total = before;
+    }
+    if (threadIdx.x == 0) kept[i] = total;
+}
+
+// ------------------------------------------------------------------ operands
+
+struct GatherArgs {
+    const void* A;
+    int64_t a_row, a_rep;
+    const int32_t* order;
+    const int* kept;
+    int64_t order_rep;
+    int base, n, d, dp;          // the chunk's first row and how many (a multiple of 64), inputs and padded
+    uint16_t *a, *at;            // parts of [m][n][dp] and of [m][d][n]; at null: none
+    int64_t a_part, at_part;
+};
+
+// 64 x 64 of the kept rows, as they are and transposed, zeros behind either end.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) head_gather_kernel(GatherArgs g) {
+    __shared__ float tile[64][65];
+    const int i = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tc = threadIdx.x & 63, tr = threadIdx.x >> 6;
+    const int kept = g.kept[i] - g.base;
+    if (r0 >= kept) return;   // no product reads them
+    const T* A = static_cast<const T*>(g.A) + i * g.a_rep;
+    constexpr bool three = sizeof(T) == 4;
+#pragma unroll 4
+    for (int q = 0; q < 16; ++q) {
+        const int r = q * 4 + tr, c = c0 + tc;
+        float v = 0.f;
+        if (r0 + r < kept && c < g.d) v = static_cast<float>(A[g.order[i * g.order_rep + g.base + r0 + r] * g.a_row + c]);
+        tile[r][tc] = v;
+        uint16_t p[3];
+        split3(v, p);
+        uint16_t* to = g.a + ((int64_t)i * g.n + r0 + r) * g.dp + c;
+        to[0] = p[0];
+        if (three) to[g.a_part] = p[1], to[2 * g.a_part] = p[2];
+    }
+    if (!g.at) return;
+    __syncthreads();
+#pragma unroll 4
+    for (int q = 0; q < 16; ++q) {
+        const int c = c0 + q * 4 + tr;
+        if (c >= g.d) continue;
+        uint16_t p[3];
+        split3(tile[tc][q * 4 + tr], p);
+        uint16_t* to = g.at + ((int64_t)i * g.d + c) * g.n + r0 + tc;
+        to[0] = p[0];
+        if (three) to[g.at_part] = p[1], to[2 * g.at_part] = p[2];
+    }
+}
+
+// W as the products read it: rows of `cp` classes (a multiple of 8, zeros behind the last), fp32 in parts.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) head_weights_kernel(const T* W, int64_t w_row, int64_t w_rep, int d, int classes, int cp,
+                                                              uint16_t* out, int64_t part) {
+    const int i = blockIdx.z;
+    for (int r = blockIdx.y; r < d; r += gridDim.y) {
+        const T* src = W + i * w_rep + r * w_row;
+        uint16_t* to = out + ((int64_t)i * d + r) * cp;
+        for (int c = (blockIdx.x * kBlock + threadIdx.x) * 8; c < cp; c += gridDim.x * kBlock * 8) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = c + e < classes ? static_cast<float>(src[c + e]) : 0.f;
+            s16x8 q[3];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint16_t p[3];
+                split3(v[e], p);
+                q[0][e] = (short)p[0]; q[1][e] = (short)p[1]; q[2][e] = (short)p[2];
+            }
+            *reinterpret_cast<s16x8*>(to + c) = q[0];
+            if (sizeof(T) == 4) {
+                *reinterpret_cast<s16x8*>(to + part + c) = q[1];
+                *reinterpret_cast<s16x8*>(to + 2 * part + c) = q[2];
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ logits
+
+struct LogitArgs {
+    const float* bias;
+    int64_t bias_rep;
+    const int32_t* label;        // kept rows' labels [m][rows]
+    const int* kept;
+    int64_t label_rep;
+    int base, n, classes, parts; // parts of a row
+    float2* stat;                // [m][n][parts] maximum and sum of exponentials, the label's class left out of the sum
+    float* z_label;              // [m][n]
+    void* e;                     // [m][n][ep] fp16 (bf16 operands) or fp32, or null
+    int64_t ep;
+};
+
+template <typename S, typename E>
+__global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, LogitArgs l) {
+    static_assert(S::BN == kWide, "a row's part is a workgroup's");
+    __shared__ __align__(1024) uint16_t lds[2 * S::kStage];
+    const TilePlace pl = tile_place(a);
+    if (pl.batch < 0) return;
+    const int kept = __builtin_amdgcn_readfirstlane(l.kept[pl.batch]) - l.base;
+    if (pl.tm * S::BM >= kept) return;
+    f32x4 acc[S::TM][S::TN];
+    tile_sums<bf16_t, S, NMajor>(a, pl, 0, a.K / kTileK, lds, acc);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w / S::WN, wn = w % S::WN;
+    const int nw = pl.tn * S::BN + wn * S::TN * 16 + (lane >> 4) * 4;
+    const float* bias = l.bias ? l.bias + pl.batch * l.bias_rep : nullptr;
+    float* red = reinterpret_cast<float*>(lds);   // [2][WN][BM], free since the last product's barrier
+    // bias, classes that do not exist, the row's maximum over the wavefront's 64 classes
+    float top[S::TM];
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) top[i] = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int n = nw + j * 16 + e;
+            const float b = bias && n < l.classes ? bias[n] : 0.f;
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i) {
+                acc[i][j][e] = n < l.classes ? acc[i][j][e] + b : -INFINITY;
+                top[i] = fmaxf(top[i], acc[i][j][e]);
+            }
+        }
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+        top[i] = fmaxf(top[i], __shfl_xor(top[i], 16));
+        top[i] = fmaxf(top[i], __shfl_xor(top[i], 32));
+        if (lane < 16) red[wn * S::BM + (wm * S::TM + i) * 16 + lane] = top[i];
+    }
+    __syncthreads();
+    float sum[S::TM];
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+        const int r = (wm * S::TM + i) * 16 + (lane & 15), m = pl.tm * S::BM + r;
+        float t = red[r];
+#pragma unroll
+        for (int k = 1; k < S::WN; ++k) t = fmaxf(t, red[k * S::BM + r]);
+        top[i] = t;
+        const float ref = t == -INFINITY ? 0.f : t;   // a part without a class left: e = 0, not NaN
+        const int y = m < kept ? l.label[pl.batch * l.label_rep + l.base + m] : -1;
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float z = acc[i][j][e];
+                v[e] = __expf(z - ref);
+                if (nw + j * 16 + e == y) l.z_label[(int64_t)pl.batch * l.n + m] = z;
+                else s += v[e];
+            }
+            const int n = nw + j * 16;
+            if (l.e && m < kept && n < l.ep) {
+                E* to = static_cast<E*>(l.e) + ((int64_t)pl.batch * l.n + m) * l.ep + n;
+                if constexpr (sizeof(E) == 4) {
+                    *reinterpret_cast<f32x4*>(to) = f32x4{v[0], v[1], v[2], v[3]};
+                } else {
+                    f16x4 h;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) h[e] = static_cast<f16_t>(v[e] * kEScale);
+                    *reinterpret_cast<f16x4*>(to) = h;
+                }
+            }
+        }
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        sum[i] = s;
+        if (lane < 16) red[(S::WN + wn) * S::BM + (wm * S::TM + i) * 16 + lane] = s;
+    }
+    __syncthreads();
+    if (wn == 0 && lane < 16) {
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i) {
+            const int r = (wm * S::TM + i) * 16 + lane, m = pl.tm * S::BM + r;
+            float s = sum[i];
+#pragma unroll
+            for (int k = 1; k < S::WN; ++k) s += red[(S::WN + k) * S::BM + r];
+            if (m < kept) l.stat[((int64_t)pl.batch * l.n + m) * l.parts + pl.tn] = make_float2(top[i], s);
+        }
+    }
+}
+
+// The parts of a row joined, a wavefront a row: its loss, the factor that makes dZ of each part's e, and the label's delta.
+__global__ void __launch_bounds__(kBlock) head_join_kernel(LogitArgs l, const int32_t* order, float e_unit, float* coef, float* delta_label,
+                                                           float* row_loss, int64_t loss_rep) {
+    const int i = blockIdx.y, lane = threadIdx.x & 63, m = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int kept = l.kept[i] - l.base;
+    if (m >= kept || m >= l.n) return;
+    const int64_t at = (int64_t)i * l.n + m;
+    const float2* st = l.stat + at * l.parts;
+    const float zy = l.z_label[at];
+    float top = zy;
+    for (int k = lane; k < l.parts; k += 64) top = fmaxf(top, st[k].x);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float others = 0.f;
+    for (int k = lane; k < l.parts; k += 64) others += st[k].y * expf((st[k].x == -INFINITY ? 0.f : st[k].x) - ref);
+    others = wave_sum(others);
+    const float ey = expf(zy - ref), whole = others + ey, unit = 1.f / whole;
+    if (coef)
+        for (int k = lane; k < l.parts; k += 64)
+            coef[at * l.parts + k] = expf((st[k].x == -INFINITY ? 0.f : st[k].x) - ref) * unit * e_unit;
+    if (lane == 0) {
+        if (coef) delta_label[at] = -others * unit;
+        // log(whole / ey); where the label's share is too small for that quotient, from the logits
+        const float loss = others < 1e20f * ey ? log1pf(others / ey) : (ref + logf(whole)) - zy;
+        row_loss[i * loss_rep + order[(int64_t)i * l.label_rep + l.base + m]] = loss;
+    }
+}
+
+__global__ void __launch_bounds__(kBlock) head_mean_kernel(const float* row_loss, int64_t loss_rep, int rows, const int* kept, float* loss) {
+    __shared__ double lds[4];
+    const int i = blockIdx.x;
+    double s = 0.0;
+    for (int r = threadIdx.x; r < rows; r += kBlock) s += row_loss[i * loss_rep + r];
+    s = wave_sum(s);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) loss[i] = kept[i] ? static_cast<float>(((lds[0] + lds[1]) + (lds[2] + lds[3])) / kept[i]) : 0.f;
+}
+
+// ------------------------------------------------------------------ dZ
+
+struct DeltaArgs {
+    const void* e;               // fp16 or fp32 [m][n][ep]
+    uint16_t* dz;                // bf16 parts [m][n][ep]; one part: e's own place
+    int64_t ep, dz_part;
+    const float *coef, *delta_label;
+    const int32_t* label;
+    const int* kept;
+    int64_t label_rep;
+    int base, n, parts, classes, row_blocks;
+    float* db_part;              // [m][row_blocks][ep]
+};
+
+// 64 rows x 2048 classes a workgroup, 8 classes a thread, so that its columns' sums stay in registers.
+template <typename E>
+__global__ void __launch_bounds__(kBlock) head_delta_kernel(DeltaArgs d) {
+    const int i = blockIdx.z, r0 = blockIdx.y * 64, c = (blockIdx.x * kBlock + threadIdx.x) * 8;
+    const int kept = d.kept[i] - d.base;
+    if (c >= d.ep) return;
+    float sum[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] = 0.f;
+    if (r0 < kept) {
+#pragma unroll 2
+        for (int r = r0; r < r0 + 64; ++r) {
+            const int64_t at = ((int64_t)i * d.n + r) * d.ep + c;
+            float v[8];
+            if (r < kept) {
+                if constexpr (sizeof(E) == 4) {
+                    const f32x4 p = *reinterpret_cast<const f32x4*>(static_cast<const float*>(d.e) + at);
+                    const f32x4 q = *reinterpret_cast<const f32x4*>(static_cast<const float*>(d.e) + at + 4);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = p[k], v[4 + k] = q[k];
+                } else {
+                    const f16x8 p = *reinterpret_cast<const f16x8*>(static_cast<const f16_t*>(d.e) + at);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = static_cast<float>(p[k]);
+                }
+                const float f = d.coef[((int64_t)i * d.n + r) * d.parts + c / kWide];
+                const int y = d.label[i * d.label_rep + d.base + r] - c;
+                const float dy = d.delta_label[(int64_t)i * d.n + r];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = k == y ? dy : v[k] * f;
+                    sum[k] += v[k];
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = 0.f;   // the last k of dW's product
+            }
+            s16x8 q[3];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                uint16_t p[3];
+                split3(v[k], p);
+                q[0][k] = (short)p[0]; q[1][k] = (short)p[1]; q[2][k] = (short)p[2];
+            }
+            *reinterpret_cast<s16x8*>(d.dz + at) = q[0];
+            if constexpr (sizeof(E) == 4) {
+                *reinterpret_cast<s16x8*>(d.dz + d.dz_part + at) = q[1];
+                *reinterpret_cast<s16x8*>(d.dz + 2 * d.dz_part + at) = q[2];
+            }
+        }
+    }
+    float* to = d.db_part + ((int64_t)i * d.row_blocks + blockIdx.y) * d.ep + c;
+    *reinterpret_cast<f32x4*>(to) = f32x4{sum[0], sum[1], sum[2], sum[3]};
+    *reinterpret_cast<f32x4*>(to + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+}
+
+// Several chunks of rows: what they have summed up so far stands in `acc` between them.  The last divides by the
+// rows that count.
+struct Across {
+    int first, last;
+    float* acc;
+    const int* kept;
+};
+__device__ __forceinline__ float per_row(const int* kept, int i) { return 1.f / static_cast<float>(max(1, kept[i])); }
+
+template <typename G>
+__global__ void __launch_bounds__(kBlock) head_db_kernel(const float* part, int row_blocks, int64_t ep, int classes, Across x, G* db,
+                                                         int64_t db_rep) {
+    const int i = blockIdx.y, c = blockIdx.x * kBlock + threadIdx.x;
+    if (c >= classes) return;
+    float s = x.first ? 0.f : x.acc[i * ep + c];
+    for (int b = 0; b < row_blocks; ++b) s += part[((int64_t)i * row_blocks + b) * ep + c];
+    if (x.last) db[i * db_rep + c] = static_cast<G>(s * per_row(x.kept, i));
+    else x.acc[i * ep + c] = s;
+}
+
+// ------------------------------------------------------------------ dA
+
+// Shares of dZ W^T over the classes, [splits][m][n][d] in 32 bits.
+template <typename S>
+__global__ void __launch_bounds__(S::kThreads) head_da_kernel(TileArgs a, float* out, int n_rows, int d) {
+    __shared__ __align__(1024) uint16_t lds[2 * S::kStage];
+    const TilePlace pl = tile_place(a);
+    if (pl.batch < 0) return;
+    int k0, k1;
+    tile_k_range(a, pl, S::BM, k0, k1);
+    if (a.m_count && pl.tm * S::BM >= __builtin_amdgcn_readfirstlane(a.m_count[pl.batch]) - a.count_base) return;
+    f32x4 acc[S::TM][S::TN];
+    tile_sums<bf16_t, S, KMajor>(a, pl, k0, k1, lds, acc);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int mw = pl.tm * S::BM + (w / S::WN) * S::TM * 16 + (lane & 15), nw = pl.tn * S::BN + (w % S::WN) * S::TN * 16 + (lane >> 4) * 4;
+    out += ((int64_t)pl.split * a.batches + pl.batch) * n_rows * d;
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+            const int m = mw + i * 16, n = nw + j * 16;
+            if (m >= a.M) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < d) out[(int64_t)m * d + n + e] = acc[i][j][e];
+        }
+}
+
+// The shares added up, each row to its place; rows that do not count get zeros.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) head_da_rows_kernel(const float* part, int splits, int m_all, int n, int d, const int32_t* order,
+                                                              int64_t order_rep, const int* kept, int base, T* dA, int64_t row, int64_t rep) {
+    const int i = blockIdx.y, r = blockIdx.x;
+    T* to = dA + i * rep + order[i * order_rep + base + r] * row;
+    const bool keep = base + r < kept[i];
+    const float unit = per_row(kept, i);
+    for (int c = threadIdx.x; c < d; c += kBlock) {
+        float s = 0.f;
+        if (keep)
+            for (int k = 0; k < splits; ++k) s += part[(((int64_t)k * m_all + i) * n + r) * d + c];
+        to[c] = static_cast<T>(s * unit);
+    }
+}
+
+// ------------------------------------------------------------------ dW
+
+template <typename S, typename G>
+__global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across x, G* dW, int64_t row, int64_t rep, int vec) {
+    __shared__ __align__(1024) uint16_t lds[2 * S::kStage];
+    const TilePlace pl = tile_place(a);
+    if (pl.batch < 0) return;
+    int k0, k1;
+    tile_k_range(a, pl, S::BM, k0, k1);
+    f32x4 acc[S::TM][S::TN];
+    tile_sums<bf16_t, S, NMajor>(a, pl, k0, k1, lds, acc);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int mw = pl.tm * S::BM + (w / S::WN) * S::TM * 16 + (lane & 15), nw = pl.tn * S::BN + (w % S::WN) * S::TN * 16 + (lane >> 4) * 4;
+    const float unit = per_row(x.kept, pl.batch);
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+            const int m = mw + i * 16, n = nw + j * 16;
+            if (m >= a.M || n >= a.N) continue;
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e];
+            float* sum = x.acc ? x.acc + ((int64_t)pl.batch * a.M + m) * a.b.len + n : nullptr;   // rows of padded classes
+            if (!x.first) {
+                const f32x4 s = *reinterpret_cast<const f32x4*>(sum);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += s[e];
+            }
+            if (!x.last) {
+                *reinterpret_cast<f32x4*>(sum) = f32x4{v[0], v[1], v[2], v[3]};
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] *= unit;
+            G* to = dW + pl.batch * rep + m * row + n;
+            if (vec && n + 4 <= a.N) {
+                if constexpr (sizeof(G) == 4) {
+                    *reinterpret_cast<f32x4*>(to) = f32x4{v[0], v[1], v[2], v[3]};
+                } else {
+                    bf16x4 h;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) h[e] = static_cast<bf16_t>(v[e]);
+                    *reinterpret_cast<bf16x4*>(to) = h;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n + e < a.N) to[e] = static_cast<G>(v[e]);
+            }
+        }
+}
+
+// ------------------------------------------------------------------ host
+
+typedef TileShape<64, 256, 1, 4> Rows64;
+typedef TileShape<128, 256, 2, 4> Rows128;
+typedef TileShape<256, 256, 2, 4> Rows256;
+
+// A product's tile by its rows: no taller than they need, 256 where there are more.
+template <typename F>
+void with_tile(TileArgs& a, F f) {
+    auto go = [&](auto shape) {
+        typedef decltype(shape) S;
+        a.mt = (a.M + S::BM - 1) / S::BM;
+        a.nt = (a.N + S::BN - 1) / S::BN;
+        f(shape);
+    };
+    if (a.M <= 64) go(Rows64());
+    else if (a.M <= 128) go(Rows128());
+    else go(Rows256());
+}
+
+struct HeadPlan {
+    bool grad, three, copy_w;    // gradients; fp32 operands in three parts; W copied first
+    int d, dp, cp, parts;        // inputs and padded, classes of a row of the copy of W, parts of a row's sum
+    int64_t ep;                  // classes of a row of e
+    int chunk, group, splits;    // rows and replicas at a time, shares of dA's product
+    int32_t *order, *label;
+    int* kept;
+    float *row_loss, *z_label, *coef, *delta_label, *da, *db_part, *db_acc, *dw_acc, *e32;
+    float2* stat;
+    uint16_t *a, *at, *w, *dz;
+    size_t bytes;
+};
+
+int head_check(const lc_head_args* h, bool grad) {
+    if (!h || h->m < 1 || h->m > kMaxReplicas || h->rows < 0 || h->inputs < 1 || h->classes < 1) return LC_ERR_ARG;
+    if (h->dtype != LC_GEMM_FP32 && h->dtype != LC_GEMM_BF16) return LC_ERR_ARG;
+    if (h->rows > LC_HEAD_MAX_ROWS || h->classes > LC_HEAD_MAX_CLASSES || h->inputs > LC_HEAD_MAX_INPUTS) return LC_ERR_UNSUPPORTED;
+    if (!h->loss || h->bias_replica < 0 || h->label_replica < 0) return LC_ERR_ARG;
+    if (h->row_loss && h->m > 1 && h->row_loss_replica < h->rows) return LC_ERR_ARG;
+    if (!aligned_to(h->loss, 4) || !aligned_to(h->row_loss, 4) || !aligned_to(h->bias, 4) || !aligned_to(h->labels, 4)) return LC_ERR_ALIGN;
+    int rc = check_input(h->W, h->m, h->inputs, h->classes, h->dtype);
+    if (rc != LC_OK) return rc;
+    if (h->rows > 0) {
+        if (!h->labels) return LC_ERR_ARG;
+        rc = check_input(h->A, h->m, h->rows, h->inputs, h->dtype);
+        if (rc != LC_OK) return rc;
+    }
+    if (!grad) return LC_OK;
+    if (h->grad_dtype != LC_GEMM_FP32 && h->grad_dtype != LC_GEMM_BF16) return LC_ERR_ARG;
+    if (h->rows > 0) rc = check_output(h->dA, h->m, h->rows, h->inputs, h->dtype);
+    if (rc == LC_OK) rc = check_output(h->dW, h->m, h->inputs, h->classes, h->grad_dtype);
+    if (rc != LC_OK) return rc;
+    if (h->db && h->m > 1 && h->db_replica < h->classes) return LC_ERR_ARG;
+    if (!aligned_to(h->db, element_bytes(h->grad_dtype))) return LC_ERR_ALIGN;
+    return LC_OK;
+}
+
+HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
+    HeadPlan p{};
+    p.grad = grad;
+    p.three = h.dtype == LC_GEMM_FP32;
+    p.d = h.inputs;
+    p.dp = static_cast<int>(round_up(h.inputs, kTileK));
+    p.parts = static_cast<int>((h.classes + kWide - 1) / kWide);
+    p.ep = round_up(h.classes, kTileK);
+    // bf16 weights are read where they stand if every row starts on 16 bytes and holds whole chunks of 8
+    p.copy_w = p.three || h.classes % 8 || !aligned_to(h.W.p, 16) || (h.inputs > 1 && h.W.row % 8) || (h.m > 1 && h.W.replica % 8) ||
+               h.W.row > kMaxRowStride;
+    p.cp = static_cast<int>(round_up(h.classes, 8));
+    // rows and replicas at a time: bytes of a row's e (fp32: and of its dZ in parts), or of its parts' sums
+    const int64_t per_row = grad ? p.ep * (p.three ? 10 : 2) : p.parts * 8;
+    const int64_t rows = round_up(std::max<int64_t>(h.rows, 1), 64);
+    const int64_t few = std::min<int64_t>(rows, 256);
+    p.group = static_cast<int>(std::min<int64_t>(h.m, std::max<int64_t>(1, kKeepBytes / (per_row * few))));
+    p.chunk = static_cast<int>(std::min<int64_t>({rows, 65536, std::max<int64_t>(few, kKeepBytes / (per_row * p.group) / 256 * 256)}));
+    const int np = p.three ? 3 : 1;
+    const int64_t g = p.group, n = p.chunk;
+    Carver c{static_cast<char*>(ws)};
+    p.order = c.take<int32_t>(h.m * h.rows);
+    p.label = c.take<int32_t>(h.m * h.rows);
+    p.kept = c.take<int>(h.m);
+    p.row_loss = c.take<float>(h.row_loss ? 0 : h.m * h.rows);
+    p.a = c.take<uint16_t>(np * g * n * p.dp);
+    p.w = c.take<uint16_t>(p.copy_w ? np * g * p.d * (int64_t)p.cp : 0);
+    p.stat = c.take<float2>(g * n * p.parts);
+    p.z_label = c.take<float>(g * n);
+    if (grad) {
+        const bool chunks = p.chunk < h.rows;
+        TileArgs t{};
+        t.M = static_cast<int>(n);
+        t.N = p.d;
+        int64_t tiles = 1;
+        with_tile(t, [&](auto) { tiles = (int64_t)t.mt * t.nt * g; });
+        // few tiles: the classes are shared out until every compute unit has a share, of 8 tiles of k at least
+        p.splits = static_cast<int>(std::max<int64_t>(1, std::min((256 + tiles - 1) / tiles, p.ep / (8 * kTileK))));
+        p.coef = c.take<float>(g * n * p.parts);
+        p.delta_label = c.take<float>(g * n);
+        p.at = c.take<uint16_t>(np * g * p.d * n);
+        p.dz = c.take<uint16_t>(np * g * n * p.ep);
+        p.e32 = c.take<float>(p.three ? g * n * p.ep : 0);
+        p.da = c.take<float>(p.splits * g * n * p.d);
+        p.db_part = c.take<float>(g * (n / 64) * p.ep);
+        p.db_acc = c.take<float>(chunks ? g * p.ep : 0);
+        p.dw_acc = c.take<float>(chunks ? g * p.d * p.ep : 0);
+    }
+    p.bytes = c.used;
+    return p;
+}
+
+// The six part products of two fp32 operands, smallest first; parts `pa` and `pb` elements apart.
+void segments(TileArgs& t, bool three, int64_t pa, int64_t pb) {
+    static const int ia[6] = {0, 1, 2, 0, 1, 0}, ib[6] = {2, 1, 0, 1, 0, 0};
+    t.segments = three ? 6 : 1;
+    for (int s = 0; s < t.segments && three; ++s) {
+        t.a.part[s] = ia[s] * pa;
+        t.b.part[s] = ib[s] * pb;
+    }
+}
+
+template <typename T, typename G>
+int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
+    const int rows = static_cast<int>(h.rows);
+    float* row_loss = h.row_loss ? h.row_loss : p.row_loss;
+    const int64_t loss_rep = h.row_loss ? h.row_loss_replica : rows;
+    head_rows_kernel<<<h.m, 1024, 0, st>>>(h.labels, h.label_replica, rows, h.classes, p.order, p.label, p.kept, row_loss, loss_rep);
+    const int64_t n = p.chunk;
+    const T *A = static_cast<const T*>(h.A.p), *W = static_cast<const T*>(h.W.p);
+    for (int g0 = 0; g0 < h.m; g0 += p.group) {
+        const int g = std::min(p.group, h.m - g0);
+        const int64_t a_part = g * n * p.dp, at_part = g * p.d * n, w_part = (int64_t)g * p.d * p.cp, dz_part = g * n * p.ep;
+        const int32_t *order = p.order + (int64_t)g0 * rows, *label = p.label + (int64_t)g0 * rows;
+        const int* kept = p.kept + g0;
+        TileOperand w{reinterpret_cast<const uint16_t*>(W + g0 * h.W.replica), h.W.row, h.W.replica, {}, p.d, h.classes};
+        if (p.copy_w) {
+            const dim3 grid(static_cast<unsigned>(std::min((p.cp + kBlock * 8 - 1) / (kBlock * 8), 64)), std::min(p.d, 2048), g);
+            head_weights_kernel<T><<<grid, kBlock, 0, st>>>(W + g0 * h.W.replica, h.W.row, h.W.replica, p.d, h.classes, p.cp, p.w, w_part);
+            w = TileOperand{p.w, p.cp, (int64_t)p.d * p.cp, {}, p.d, p.cp};
+        }
+        const int chunks = rows ? static_cast<int>((rows + n - 1) / n) : p.grad ? 1 : 0;   // no rows: gradients of zero
+        for (int k = 0; k < chunks; ++k) {
+            const int base = static_cast<int>(k * n), here = static_cast<int>(std::min<int64_t>(n, rows - base));
+            const GatherArgs ga{A + g0 * h.A.replica, h.A.row, h.A.replica, order, kept, rows, base, static_cast<int>(n), p.d, p.dp, p.a,
+                                p.grad ? p.at : nullptr, a_part, at_part};
+            if (here) head_gather_kernel<T><<<dim3(p.dp / 64, (here + 63) / 64, g), kBlock, 0, st>>>(ga);
+            TileArgs t{};
+            t.a = TileOperand{p.a, p.dp, n * p.dp, {}, here, p.dp};
+            t.b = w;
+            segments(t, p.three, a_part, w_part);
+            t.M = here;
+            t.N = h.classes;
+            t.K = p.dp;
+            t.batches = g;
+            t.splits = 1;
+            const LogitArgs l{h.bias ? h.bias + g0 * h.bias_replica : nullptr, h.bias_replica, label, kept, rows, base, static_cast<int>(n),
+                              h.classes, p.parts, p.stat, p.z_label, p.grad ? (p.three ? (void*)p.e32 : (void*)p.dz) : nullptr, p.ep};
+            typedef typename std::conditional<sizeof(T) == 4, float, f16_t>::type E;
+            if (here) {
+                with_tile(t, [&](auto s) {
+                    typedef decltype(s) S;
+                    head_logits_kernel<S, E><<<tile_grid(t), S::kThreads, 0, st>>>(t, l);
+                });
+                head_join_kernel<<<dim3((here + 3) / 4, g), kBlock, 0, st>>>(l, order, p.three ? 1.f : 1.f / kEScale, p.coef,
+                                                                            p.delta_label, row_loss + g0 * loss_rep, loss_rep);
+            }
+            if (!p.grad) continue;
+            const int row_blocks = (here + 63) / 64;
+            const DeltaArgs da{l.e, p.dz, p.ep, dz_part, p.coef, p.delta_label, label, kept, rows, base, static_cast<int>(n), p.parts,
+                               h.classes, row_blocks, p.db_part};
+            if (here) head_delta_kernel<E><<<dim3(static_cast<unsigned>((p.ep + kBlock * 8 - 1) / (kBlock * 8)), row_blocks, g), kBlock, 0, st>>>(da);
+            Across x{k == 0, k + 1 == chunks, p.db_acc, kept};
+            if (h.db)
+                head_db_kernel<G><<<dim3((h.classes + kBlock - 1) / kBlock, g), kBlock, 0, st>>>(
+                    p.db_part, row_blocks, p.ep, h.classes, x, static_cast<G*>(h.db) + g0 * h.db_replica, h.db_replica);
+            // dA = dZ W^T
+            t = TileArgs{};
+            t.a = TileOperand{p.dz, p.ep, n * p.ep, {}, here, static_cast<int>(p.ep)};
+            t.b = w;
+            segments(t, p.three, dz_part, w_part);
+            t.M = here;
+            t.N = p.d;
+            t.K = static_cast<int>(p.ep);
+            t.batches = g;
+            t.splits = p.splits;
+            t.m_count = kept;
+            t.count_base = base;
+            if (here) {
+                with_tile(t, [&](auto s) {
+                    typedef decltype(s) S;
+                    head_da_kernel<S><<<tile_grid(t), S::kThreads, 0, st>>>(t, p.da, static_cast<int>(n), p.d);
+                });
+                head_da_rows_kernel<T><<<dim3(here, g), kBlock, 0, st>>>(p.da, p.splits, g, static_cast<int>(n), p.d, order, rows, kept, base,
+                                                                         static_cast<T*>(h.dA.p) + g0 * h.dA.replica, h.dA.row, h.dA.replica);
+            }
+            // dW = A^T dZ
+            t = TileArgs{};
+            t.a = TileOperand{p.at, n, p.d * n, {}, p.d, static_cast<int>(n)};
+            t.b = TileOperand{p.dz, p.ep, n * p.ep, {}, static_cast<int>(n), static_cast<int>(p.ep)};
+            segments(t, p.three, at_part, dz_part);
+            t.M = p.d;
+            t.N = h.classes;
+            t.K = static_cast<int>(round_up(here, kTileK));
+            t.batches = g;
+            t.splits = 1;
+            t.k_count = kept;
+            t.count_base = base;
+            x.acc = p.dw_acc;
+            G* dW = static_cast<G*>(h.dW.p) + g0 * h.dW.replica;
+            const size_t gb = 4 * sizeof(G);
+            const int vec = aligned_to(dW, gb) && h.dW.row % 4 == 0 && (h.m == 1 || h.dW.replica % 4 == 0);
+            with_tile(t, [&](auto s) {
+                typedef decltype(s) S;
+                head_dw_kernel<S, G><<<tile_grid(t), S::kThreads, 0, st>>>(t, x, dW, h.dW.row, h.dW.replica, vec);
+            });
+        }
+    }
+    head_mean_kernel<<<h.m, kBlock, 0, st>>>(row_loss, loss_rep, rows, p.kept, h.loss);
+    return hipGetLastError() == hipSuccess ? LC_OK : LC_ERR_HIP;
+}
+
+int head(const lc_head_args* h, bool grad, void* ws, size_t ws_bytes, void* stream) {
+    const int rc = head_check(h, grad);
+    if (rc != LC_OK) return rc;
+    const HeadPlan p = head_plan(*h, grad, ws);
+    if (!ws || ws_bytes < p.bytes) return LC_ERR_WORKSPACE;
+    if (!aligned_to(ws, 256)) return LC_ERR_ALIGN;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool g16 = grad && h->grad_dtype == LC_GEMM_BF16;
+    if (h->dtype == LC_GEMM_BF16) return g16 ? run_head<bf16_t, bf16_t>(*h, p, st) : run_head<bf16_t, float>(*h, p, st);
+    return g16 ? run_head<float, bf16_t>(*h, p, st) : run_head<float, float>(*h, p, st);
+}
+
+}  // namespace
+}  // namespace lc
+
+using namespace lc;
+
+extern "C" {
+
+size_t lc_softmax_head_workspace_bytes(const lc_head_args* h, int with_grad) {
+    if (head_check(h, with_grad != 0) != LC_OK) return 0;
+    return head_plan(*h, with_grad != 0, nullptr).bytes;
+}
+int lc_softmax_head_loss(const lc_head_args* h, void* workspace, size_t workspace_bytes, void* stream) {
+    return head(h, false, workspace, workspace_bytes, stream);
+}
+int lc_softmax_head_grad(const lc_head_args* h, void* workspace, size_t workspace_bytes, void* stream) {
+    return head(h, true, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,284 @@
+"""lc_orthogonalize, lc_update_orthogonal and lc_update_from_grad_orthogonal against the formulas in 64 bits.
+
+Tolerance.  Step k commits an error of Frobenius norm
+  e_k <= (|a| u + (|b| + 2 |c| s) (2 q) s + q (|b| s + |c| s^3) ...) |X_k|_F,   s = |X_k|_2,
+q the relative error of a product of stored factors (fp32: 2^-21 and the sum over k terms in 32 bits, 2^-24 sqrt(k);
+one fp16 part: two roundings of 2^-11), and what comes after multiplies it, in the basis of the singular vectors, by divided
+differences of the remaining polynomial g at the singular values: (g(s_i) -+ g(s_j)) / (s_i -+ s_j), and g(s) / s for the
+directions that are missing.  Their largest bounds what arrives; singular values are taken from the 64-bit run."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+A_, B_, C_ = 3.4445, -4.7750, 2.0315
+
+
+@pytest.fixture(scope="module")
+def pkg():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    import paper_1810_08313_amd as p
+    p.lib()
+    return p
+
+
+def _poly(s):
+    return A_ * s + B_ * s ** 3 + C_ * s ** 5
+
+
+def _reference(M, steps, one_part):
+    """O of one matrix (CPU, 64 bits) and the bound of the Frobenius norm of what the kernels may be off by."""
+    import torch
+    M = M.double().cpu()
+    if not float(M.norm()):
+        return M, 0.0
+    X = M / M.norm()
+    u, s, vt = torch.linalg.svd(X, full_matrices=False)
+    k = max(M.shape)
+    q = (2.0 ** -10 if one_part else 2.0 ** -21) + U * np.sqrt(k)
+    sv, tol = [s], 0.0
+    for _ in range(steps):
+        sv.append(_poly(sv[-1]))
+
+    def rest(x, j):
+        for _ in range(j):
+            x = _poly(x)
+        return x
+    for i in range(steps):
+        x, top, fro = sv[i], float(sv[i].max()), float(sv[i].norm())
+        # errors of A (twice, in b A and in A A), of A A, of B X, of a X
+        e = (4 * U * A_ + q * (abs(B_) * top ** 2 * 2 + C_ * top ** 4 * 4)) * fro + 4 * U * fro
+        y, j = sv[i + 1], steps - i - 1
+        amp = 1.0
+        if j:
+            a, b = y[:, None], y[None, :]
+            fa, fb = rest(a, j), rest(b, j)
+            minus, plus = (fa - fb).abs() / (a - b).abs().clamp(min=1e-9), (fa + fb).abs() / (a + b).abs().clamp(min=1e-9)
+            zero = A_ ** j if float(y.min()) < 1e-3 or M.shape[0] == M.shape[1] else float((rest(y, j) / y).abs().max())
+            h = 1e-6
+            slope = ((rest(y + h, j) - rest(y - h, j)) / (2 * h)).abs().max()
+            near = (a - b).abs() > 1e-6
+            amp = max(float((minus * near).max()), float(plus.max()), float(slope), float((rest(y, j) / y.clamp(min=1e-9)).abs().max()),
+                      zero if float(y.min()) < 1e-3 else 0.0)
+        tol += amp * e
+    start = 4 * U * max(float((rest(sv[0], steps) / sv[0].clamp(min=1e-9)).abs().max()), 1.0)
+    return (u * sv[-1]) @ vt, tol + start
+
+
+def _matrix(m, rows, cols, seed, kind):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rn = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    if kind == "plain":
+        return rn(m, rows, cols)
+    k = max(1, min(rows, cols) // 4)       # a few directions and noise far below them
+    return torch.stack([rn(rows, k) @ rn(k, cols) for _ in range(m)]) + 1e-3 * rn(m, rows, cols)
+
+
+def _one_part(t, rows, cols):
+    import torch
+    return t == torch.bfloat16 and min(rows, cols) > 384
+
+
+def _check(name, got, want, tol):
+    import torch
+    half = torch.finfo(torch.bfloat16).eps / 2 if got.dtype == torch.bfloat16 else U
+    off = float((got.double().cpu() - want).norm())
+    lim = tol + half * (float(want.norm()) + tol)
+    print(f"  {name}: off {off:.3e} of {float(want.norm()):.3e}, bound {lim:.3e}", flush=True)
+    assert off <= lim, (name, off, lim)
+
+
+SIZES = [(1, 1, 1), (2, 1, 9), (2, 7, 1), (3, 10, 40), (2, 64, 64), (2, 65, 130), (1, 130, 65), (2, 100, 300), (1, 257, 255), (1, 385, 400),
+         (1, 520, 390), (1, 400, 1030), (5, 30, 1000)]
+
+
+@pytest.mark.parametrize("kind", ["plain", "few"])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("m,rows,cols", SIZES)
+def test_sizes(pkg, m, rows, cols, bf16, kind):
+    import torch
+    t = torch.bfloat16 if bf16 else torch.float32
+    M = _matrix(m, rows, cols, rows * 3 + cols, kind).to(t)
+    print(f"orthogonalize m={m} {rows}x{cols} {t} {kind}", flush=True)
+    out = pkg.orthogonalize(M)
+    torch.cuda.synchronize()
+    for i in range(m):
+        want, tol = _reference(M[i], 5, _one_part(t, rows, cols))
+        _check(f"replica {i}", out[i], want, tol)
+
+
+@pytest.mark.parametrize("shape", [(1, 1100, 1200), (20, 520, 530), (2, 2100, 700)])
+def test_larger_tiles(pkg, shape):
+    """The tiles of 128 and 256, chosen by the number of workgroups; odd sizes on both sides."""
+    import torch
+    for t in (torch.float32, torch.bfloat16):
+        M = _matrix(*shape, 7, "few").to(t)
+        print(f"orthogonalize {shape} {t}", flush=True)
+        out = pkg.orthogonalize(M)
+        torch.cuda.synchronize()
+        for i in (0, shape[0] - 1):
+            want, tol = _reference(M[i], 5, _one_part(t, *shape[1:]))
+            _check(f"replica {i}", out[i], want, tol)
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 8])
+def test_steps(pkg, steps):
+    M = _matrix(2, 60, 90, 3, "plain")
+    out = pkg.orthogonalize(M, steps)
+    for i in range(2):
+        want, tol = _reference(M[i], steps, False)
+        _check(f"replica {i}", out[i], want, tol)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_values(pkg, bf16):
+    """A zero matrix, sizes far from one, and elements that are not finite: each stays in its replica."""
+    import torch
+    t = torch.bfloat16 if bf16 else torch.float32
+    M = _matrix(6, 40, 50, 5, "plain").to(t)
+    base = pkg.orthogonalize(M)
+    M[1] = 0
+    M[2] *= 2.0 ** 60
+    M[3] *= 2.0 ** -90
+    M[4, 3, 3] = float("inf")
+    M[5, 0, 0] = float("nan")
+    out = pkg.orthogonalize(M)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], base[0]) and not out[1].any()
+    # a power of two changes no digit of the matrix and at most the last of 1 / |M|, a relative U of X_0
+    for i in (2, 3):
+        want, tol = _reference(M[i], 5, False)
+        _check(f"replica {i}", out[i], want, tol)
+    assert bool(out[4].isnan().any()) and bool(out[5].isnan().all())
+
+
+def test_places(pkg):
+    """Matrices inside rows of a larger array, replicas interleaved, the result where the matrix stands."""
+    import torch
+    for t, rows, cols in ((torch.float32, 70, 33), (torch.bfloat16, 20, 90)):
+        M = _matrix(3, rows, cols, 9, "plain").to(t)
+        want = pkg.orthogonalize(M)
+        big = torch.full((rows, 3, cols + 7), 2.0, device="cuda", dtype=t)
+        v = big.transpose(0, 1)[:, :, 3:3 + cols]
+        v.copy_(M)
+        assert torch.equal(pkg.orthogonalize(v), want)
+        pkg.orthogonalize(v, out=v)
+        torch.cuda.synchronize()
+        assert torch.equal(v, want) and bool((big[:, :, :3] == 2.0).all()) and bool((big[:, :, 3 + cols:] == 2.0).all())
+
+
+def _update_reference(X, V, G, lr, beta, wd, rows, cols):
+    v = beta * V.double().cpu() + G.double().cpu()
+    o, tol = _reference(v.float(), 5, False)
+    s = max(1.0, cols / rows) ** 0.5
+    x = X.double().cpu()
+    return x - lr * (s * o + wd * x), v, lr * s * (tol + 4 * U * float(o.norm())) + 2 * U * float(x.norm())
+
+
+@pytest.mark.parametrize("beta,wd", [(0.9, 1e-3), (0.0, 0.0)])
+@pytest.mark.parametrize("m,rows,cols", [(1, 1, 1), (2, 12, 30), (3, 65, 20), (2, 130, 260), (1, 301, 150)])
+def test_update(pkg, m, rows, cols, beta, wd):
+    import torch
+    P = rows * cols + 5
+    X, V, G = (_matrix(m, 1, P, k, "plain")[:, 0] for k in (1, 2, 3))
+    if beta == 0.0:
+        V.fill_(float("nan"))        # not read
+    x0, v0 = X.clone(), V.clone()
+    at = [t.as_strided((m, rows, cols), (P, cols, 1), 3) for t in (X, V, G)]
+    start = [t.clone() for t in at]
+    if beta == 0.0:
+        start[1].zero_()
+    pkg.update_orthogonal(*at, 0.02, beta, wd)
+    torch.cuda.synchronize()
+    for i in range(m):
+        x, v, tol = _update_reference(*(t[i] for t in start), 0.02, beta, wd, rows, cols)
+        assert bool(((at[1][i].double().cpu() - v).abs() <= 2 * U * (v.abs() + start[1][i].double().cpu().abs() + 1)).all())
+        _check(f"replica {i}", at[0][i], x, tol)
+    for t, old in ((X, x0), (V, v0)):
+        keep = torch.ones(P, dtype=torch.bool, device="cuda")
+        keep[3:3 + rows * cols] = False
+        assert bool((t[:, keep] == old[:, keep]).all() or (beta == 0.0 and t is V))
+
+
+def test_update_from_grad_orthogonal(pkg):
+    """A run's update from explicit gradients: matrices along the orthogonalised momentum, biases as lc_update_from_grad; twice,
+    the second time with a broadcast pending; the padding stays zero and the counter where it is."""
+    import torch
+    import synth
+    dims, m = [70, 33, 130, 10], 3
+    md = pkg.make_model(pkg.KIND_MLP, dims, B=8, N=64, E=16, lr=0.05, beta=0.9, wd=1e-3)
+    w = synth.make_workload("cfg2", N=64, m=m, dims=dims, E=16)
+    run = pkg.LocalSGD(m, md, 5, w.x1, w.data, w.labels)
+    with pytest.raises(pkg.LcError):
+        run.update_from_grad_orthogonal()        # no gradient set
+    g = np.random.default_rng(3)
+    for k in range(2):
+        if k:
+            run.set_lazy_broadcast(True)
+            run.average()
+        X, V, it = run.get_state()
+        if k:
+            run.average()                        # pending again: get_state has written the rows
+        G = g.standard_normal(X.shape).astype(np.float32)
+        run.set_grad(G)
+        run.update_from_grad_orthogonal()
+        X2, V2, it2 = run.get_state()
+        assert it2 == it and not run.X[:, run.P:].any() and not run.V[:, run.P:].any()
+        off = 0
+        for a, b in zip(dims[:-1], dims[1:]):
+            for i in range(m):
+                mat = lambda t: torch.from_numpy(t[i, off:off + a * b].reshape(a, b).copy())  # noqa: E731
+                x, v, tol = _update_reference(mat(X), mat(V), mat(G), 0.05, 0.9, 1e-3, a, b)
+                assert np.abs(mat(V2).double() - v).max() <= 4 * U * float(v.abs().max())
+                _check(f"step {k} layer {a}-{b} replica {i}", mat(X2), x, tol)
+            s = slice(off + a * b, off + a * b + b)
+            gb = G[:, s].astype(np.float64) + np.float64(np.float32(1e-3)) * X[:, s]
+            vb = np.float64(np.float32(0.9)) * V[:, s] + gb
+            xb = X[:, s] - np.float64(np.float32(0.05)) * vb
+            assert np.abs(V2[:, s] - vb).max() <= 8 * U * (1 + np.abs(vb).max()) and np.abs(X2[:, s] - xb).max() <= 8 * U * (1 + np.abs(xb).max())
+            off += a * b + b
+    run.close()
+
+
+def test_streams_graph_and_repeats(pkg):
+    import torch
+    M = _matrix(2, 150, 300, 3, "plain")
+    ref = pkg.orthogonalize(M).clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    a, b = pkg.orthogonalize(M, stream=side), pkg.orthogonalize(M)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(a, ref) and torch.equal(b, ref)
+    X, V, G = _matrix(2, 90, 60, 4, "plain"), _matrix(2, 90, 60, 5, "plain"), _matrix(2, 90, 60, 6, "plain")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = pkg.orthogonalize(M)
+        pkg.update_orthogonal(X, V, G, 0.1, 0.9)
+    for k in range(3):
+        M.mul_(1.5).add_(0.1)
+        x, v = X.clone(), V.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = pkg.orthogonalize(M)
+        pkg.update_orthogonal(x, v, G, 0.1, 0.9)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(X, x) and torch.equal(V, v)
+
+
+def test_bindings_refuse(pkg):
+    import torch
+    M = _matrix(2, 8, 12, 1, "plain")
+    bad = [lambda: pkg.orthogonalize(M.half()), lambda: pkg.orthogonalize(M[0]), lambda: pkg.orthogonalize(M, 0), lambda: pkg.orthogonalize(M, 17),
+           lambda: pkg.orthogonalize(M, out=M.bfloat16()), lambda: pkg.update_orthogonal(M, M, M, 0.1, 0.9),
+           lambda: pkg.update_orthogonal(M.bfloat16(), M, M, 0.1, 0.9), lambda: pkg.update_orthogonal(M, M.clone(), M.clone(), 0.0, 0.9)]
+    for f in bad:
+        with pytest.raises(pkg.LcError):
+            f()
+    quad = pkg.LocalSGD(2, pkg.make_model(pkg.KIND_QUAD, [64]), 0, qa=np.ones((2, 64), np.float32), qc=np.zeros((2, 64), np.float32))
+    quad.set_grad(np.zeros((2, 64), np.float32))
+    with pytest.raises(pkg.LcError):
+        quad.update_from_grad_orthogonal()
+    quad.close()
