@@ -143,7 +143,7 @@ __device__ __forceinline__ void store_factors(const Factors& f, int64_t at, cons
 
 template <typename S, BLayout LB, OrthStep STEP>
 __global__ void __launch_bounds__(S::kThreads) orth_product_kernel(TileArgs a, OrthOut o) {
-    __shared__ __align__(1024) uint16_t lds[2 * S::kStage];
+    __shared__ __align__(1024) uint16_t lds[S::kLds];
     const TilePlace pl = tile_place(a);
     if (pl.batch < 0) return;
     f32x4 acc[S::TM][S::TN];
@@ -213,9 +213,9 @@ __global__ void __launch_bounds__(S::kThreads) orth_product_kernel(TileArgs a, O
     }
 }
 
-typedef TileShape<256, 256, 2, 4> Large;
-typedef TileShape<128, 128, 2, 2> Medium;
-typedef TileShape<64, 64, 2, 2> Small;
+typedef TileShape<256, 256, 2, 4, 2> Large;
+typedef TileShape<128, 128, 2, 2, 2> Medium;
+typedef TileShape<64, 64, 2, 2, 4> Small;
 
 template <typename S>
 void launch_product(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t st) {

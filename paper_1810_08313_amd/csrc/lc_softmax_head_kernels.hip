@@ -174,7 +174,7 @@ struct LogitArgs {
 template <typename S, typename E>
 __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, LogitArgs l) {
     static_assert(S::BN == kWide, "a row's part is a workgroup's");
-    __shared__ __align__(1024) uint16_t lds[2 * S::kStage];
+    __shared__ __align__(1024) uint16_t lds[S::kLds];
     const TilePlace pl = tile_place(a);
     if (pl.batch < 0) return;
     const int kept = __builtin_amdgcn_readfirstlane(l.kept[pl.batch]) - l.base;
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(kBlock) head_db_kernel(const float* part, int 
 // Shares of dZ W^T over the classes, [splits][m][n][d] in 32 bits.
 template <typename S>
 __global__ void __launch_bounds__(S::kThreads) head_da_kernel(TileArgs a, float* out, int n_rows, int d) {
-    __shared__ __align__(1024) uint16_t lds[2 * S::kStage];
+    __shared__ __align__(1024) uint16_t lds[S::kLds];
     const TilePlace pl = tile_place(a);
     if (pl.batch < 0) return;
     int k0, k1;
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(kBlock) head_da_rows_kernel(const float* part,
 
 template <typename S, typename G>
 __global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across x, G* dW, int64_t row, int64_t rep, int vec) {
-    __shared__ __align__(1024) uint16_t lds[2 * S::kStage];
+    __shared__ __align__(1024) uint16_t lds[S::kLds];
     const TilePlace pl = tile_place(a);
     if (pl.batch < 0) return;
     int k0, k1;
@@ -489,9 +489,9 @@ __global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across
 
 // ------------------------------------------------------------------ host
 
-typedef TileShape<64, 256, 1, 4> Rows64;
-typedef TileShape<128, 256, 2, 4> Rows128;
-typedef TileShape<256, 256, 2, 4> Rows256;
+typedef TileShape<64, 256, 1, 4, 2> Rows64;
+typedef TileShape<128, 256, 2, 4, 3> Rows128;
+typedef TileShape<256, 256, 2, 4, 2> Rows256;
 
 // A product's tile by its rows: no taller than they need, 256 where there are more.
 template <typename F>

@@ -8,7 +8,7 @@
 // 16-bit parts, and a product of two such sums is a list of part products over one accumulator.
 //
 // A workgroup owns a BM x BN tile.  Tiles of 64 k of both operands go from global memory straight into
-// LDS (16 bytes a lane, no registers), two buffers in turn.  16-byte chunks are permuted inside a row,
+// LDS (16 bytes a lane, no registers), into two to four buffers in turn.  16-byte chunks are permuted inside a row,
 // by permuting what each lane fetches, so that the operand reads of a wavefront spread over all banks:
 //   KMajor  row of 64 k = 8 chunks:    chunk c of row r at c ^ ((r >> 1) & 7)
 //   NMajor  row of BN n, 32-byte pairs: pair p of row k at p ^ ((k & 3) | (k >> 3 & 1) << 2), as far as there are pairs
@@ -61,12 +61,15 @@ struct TileArgs {
 
 enum BLayout { KMajor, NMajor };
 
-template <int BM_, int BN_, int WM_, int WN_>
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
 struct TileShape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;   // WM x WN wavefronts
     static constexpr int kThreads = 64 * WM * WN;
     static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;     // 16 x 16 tiles of a wavefront
     static constexpr int kStage = (BM + BN) * kTileK;              // elements of one LDS buffer
+    static constexpr int kStages = STAGES_, kLds = kStages * kStage;
+    static constexpr int kLoads = kStage / 8 / kThreads;           // load instructions of a thread for a buffer
+    static_assert(kStage % (8 * kThreads) == 0 && kLoads * (kStages - 2) < 64, "what a wait can count");
 };
 
 typedef __attribute__((address_space(3))) void* LdsPtr;
@@ -100,9 +103,9 @@ struct KMajorFetch {
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) fetch16(at, off[q], to + q * kPer * kTileK);
         } else {
-            const int back = max(0, k0 + c8 + 8 - o.len);   // k0 < len, both multiples of 8: it stays inside the tile
+            const int k = min(k0 + c8, o.len - 8);
 #pragma unroll
-            for (int q = 0; q < kLoads; ++q) fetch16(at, off[q] - 2u * (uint32_t)back, to + q * kPer * kTileK);
+            for (int q = 0; q < kLoads; ++q) fetch16(base, off[q] + 2u * (uint32_t)(k - c8), to + q * kPer * kTileK);
         }
     }
 };
@@ -133,10 +136,12 @@ struct NMajorFetch {
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) fetch16(at, off[q], to + q * THREADS * 8);
         } else {
+            const int first = min(k0, o.rows - 1);
+            at = base + (int64_t)first * row2;
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) {
-                const int back = max(0, q * kPer + k + k0 + 1 - o.rows);   // k0 < rows: at most q * kPer + k
-                fetch16(at, off[q] - (uint32_t)back * row2, to + q * THREADS * 8);
+                const int kk = q * kPer + k;
+                fetch16(at, off[q] - (uint32_t)(kk - (min(k0 + kk, o.rows - 1) - first)) * row2, to + q * THREADS * 8);
             }
         }
     }
@@ -209,10 +214,23 @@ inline unsigned tile_grid(const TileArgs& a) {
 
 // The sums of one tile.  On return acc[i][j][e] of lane l of wavefront (wm, wn) is row
 // wm * TM * 16 + 16 i + (l & 15), column wn * TN * 16 + 16 j + 4 (l >> 4) + e of the tile.
+//
+// kStages buffers: a tile of k is asked for kStages - 1 tiles ahead, and what is waited for is the oldest only.
+// With eight wavefronts, two share a SIMD: the second half runs one barrier behind the first, so that one of the two
+// feeds the matrix cores while the other reads its operands.
+constexpr int kWaitLds = 0xC07F;   // s_waitcnt: all LDS reads, nothing else
+constexpr int wait_loads(int n) { return (n & 15) | (n >> 4) << 14 | 0x0F70; }   // all but n loads
+
+__device__ __forceinline__ void tile_barrier() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 template <typename T, typename S, BLayout L>
 __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl, int kt0, int kt1, uint16_t* lds,
                                           f32x4 (&acc)[S::TM][S::TN]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WN, wn = wave % S::WN;
     const int m0 = pl.tm * S::BM, n0 = pl.tn * S::BN;
     const int per_seg = kt1 - kt0, total = per_seg * a.segments;
@@ -223,50 +241,117 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
     if (total <= 0) return;
     const char* ab = reinterpret_cast<const char*>(a.a.p + (int64_t)pl.batch * a.a.batch + (int64_t)m0 * a.a.row);
     const char* bb = reinterpret_cast<const char*>(a.b.p + (int64_t)pl.batch * a.b.batch + (L == KMajor ? (int64_t)n0 * a.b.row : 0));
-    KMajorFetch<S::BM, S::kThreads> fa_;
-    typename FetchB<L, S::BN, S::kThreads>::type fb_;
-    fa_.init(a.a, m0);
-    fb_.init(a.b, n0);
-    int seg = 0, next_k = kt0;   // of the tile that is fetched next
-    auto fetch = [&](uint16_t* to) {
-        fa_.fetch(a.a, ab + 2 * a.a.part[seg], next_k * kTileK, to);
-        fb_.fetch(a.b, bb + 2 * a.b.part[seg], next_k * kTileK, to + S::BM * kTileK);
+    KMajorFetch<S::BM, S::kThreads> fetch_a;
+    typename FetchB<L, S::BN, S::kThreads>::type fetch_b;
+    fetch_a.init(a.a, m0);
+    fetch_b.init(a.b, n0);
+    constexpr int NS = S::kStages;
+    int seg = 0, next_k = kt0, next_buf = 0;   // of the tile that is fetched next
+    auto ask_a = [&] { fetch_a.fetch(a.a, ab + 2 * a.a.part[seg], next_k * kTileK, lds + next_buf * S::kStage); };
+    auto ask_b = [&] {
+        fetch_b.fetch(a.b, bb + 2 * a.b.part[seg], next_k * kTileK, lds + next_buf * S::kStage + S::BM * kTileK);
         if (++next_k == kt1) next_k = kt0, ++seg;
+        next_buf = next_buf + 1 == NS ? 0 : next_buf + 1;
     };
     const int rescale_at = a.rescale_after ? a.rescale_after * per_seg : -1;
-    fetch(lds);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    for (int t = 0; t < total; ++t) {
-        uint16_t* cur = lds + (t & 1) * S::kStage;
-        if (t + 1 < total) fetch(lds + ((t + 1) & 1) * S::kStage);
-        if (t == rescale_at) {
+    const int ahead = min(NS - 1, total);
+    for (int t = 0; t < ahead; ++t) {
+        ask_a();
+        ask_b();
+    }
+    int buf = 0;
+    // a quarter of the wavefront's tile at a time: half of its rows by half of its columns, both 32-deep steps
+    constexpr int HM = S::TM / 2, HN = S::TN / 2;
+    s16x8 fa[HM][2], fb[2][HN][2];
+    auto read_b = [&](const uint16_t* tb, int h) {
 #pragma unroll
-            for (int i = 0; i < S::TM; ++i)
+        for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-                for (int j = 0; j < S::TN; ++j) acc[i][j] *= a.rescale;
-        }
-        const uint16_t* ta = cur + wm * S::TM * 16 * kTileK;
-        const uint16_t* tb = cur + S::BM * kTileK;
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            s16x8 fa[S::TM], fb[S::TN];
-#pragma unroll
-            for (int j = 0; j < S::TN; ++j) {
+            for (int j = 0; j < HN; ++j) {
                 if constexpr (L == KMajor)
-                    fb[j] = read_kmajor(tb, (wn * S::TN + j) * 16, ks, lane);
+                    fb[h][j][ks] = read_kmajor(tb, (wn * S::TN + h * HN + j) * 16, ks, lane);
                 else
-                    fb[j] = read_nmajor<S::BN>(tb, (wn * S::TN + j) * 16, ks, lane);
+                    fb[h][j][ks] = read_nmajor<S::BN>(tb, (wn * S::TN + h * HN + j) * 16, ks, lane);
             }
+    };
+    auto read_a = [&](const uint16_t* ta, int h) {
 #pragma unroll
-            for (int i = 0; i < S::TM; ++i) fa[i] = read_kmajor(ta, i * 16, ks, lane);
+        for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int i = 0; i < S::TM; ++i)
+            for (int i = 0; i < HM; ++i) fa[i][ks] = read_kmajor(ta, (wm * S::TM + h * HM + i) * 16, ks, lane);
+    };
+    auto mma = [&](int hm, int hn) {
 #pragma unroll
-                for (int j = 0; j < S::TN; ++j) acc[i][j] = mma32(T(), fb[j], fa[i], acc[i][j]);
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int i = 0; i < HM; ++i)
+#pragma unroll
+                for (int j = 0; j < HN; ++j)
+                    acc[hm * HM + i][hn * HN + j] = mma32(T(), fb[hn][j][ks], fa[i][ks], acc[hm * HM + i][hn * HN + j]);
+    };
+    auto turn = [&](int hm, int hn) {   // operands are there: this half's turn at the matrix cores
+        __builtin_amdgcn_s_waitcnt(kWaitLds);
+        tile_barrier();
+        __builtin_amdgcn_s_setprio(1);
+        mma(hm, hn);
+        __builtin_amdgcn_s_setprio(0);
+        tile_barrier();
+    };
+    auto rescale = [&] {
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) acc[i][j] *= a.rescale;
+    };
+    auto oldest = [&](int asked) {   // tiles asked for beyond the one that is waited for
+        if (asked == NS - 2) __builtin_amdgcn_s_waitcnt(wait_loads((NS - 2) * S::kLoads));
+        else __builtin_amdgcn_s_waitcnt(wait_loads(0));
+    };
+    if constexpr (S::WM * S::WN == 8) {
+        const bool late = wave >= 4;
+        oldest(ahead - 1);
+        tile_barrier();
+        if (late) tile_barrier();
+        for (int t = 0; t < total; ++t) {
+            const uint16_t *ta = lds + buf * S::kStage, *tb = ta + S::BM * kTileK;
+            buf = buf + 1 == NS ? 0 : buf + 1;
+            const bool more = t + NS - 1 < total;
+            if (t == rescale_at) rescale();
+            read_b(tb, 0);
+            read_a(ta, 0);
+            if (more) ask_a();
+            turn(0, 0);
+            read_b(tb, 1);
+            if (more) ask_b();
+            turn(0, 1);
+            read_a(ta, 1);
+            turn(1, 1);
+            oldest(more ? NS - 2 : 0);
+            turn(1, 0);
         }
-        __builtin_amdgcn_s_waitcnt(0);   // the next tile is in LDS, this one's reads are done
-        __syncthreads();
+        if (!late) tile_barrier();
+    } else {
+        for (int t = 0; t < total; ++t) {
+            oldest(min(total - t, NS - 1) - 1);
+            tile_barrier();   // the tile is there, and all have read the one whose place is filled next
+            const uint16_t *ta = lds + buf * S::kStage, *tb = ta + S::BM * kTileK;
+            buf = buf + 1 == NS ? 0 : buf + 1;
+            if (t + NS - 1 < total) {
+                ask_a();
+                ask_b();
+            }
+            if (t == rescale_at) rescale();
+            read_b(tb, 0);
+            read_a(ta, 0);
+            read_b(tb, 1);
+            mma(0, 0);
+            mma(0, 1);
+            read_a(ta, 1);
+            mma(1, 1);
+            mma(1, 0);
+            __builtin_amdgcn_s_waitcnt(kWaitLds);
+        }
+        tile_barrier();
     }
 }
 
