@@ -8,15 +8,15 @@
 //
 // Bound by the products, 2 S S L + (S S S + S S L) multiply-adds a step for S x L: A and A A are symmetric, only tiles
 // on and above the diagonal are formed and stored twice.  The products run on the 16-bit matrix cores.  All factors
-// are bounded (|X| <= 1.3, |A| <= 1.7, |B| <= 13 in the spectral norm, so in every element), which is what fp16 wants:
-// they are stored times 2^10, with 11 significant bits down to 6e-8.
+// are bounded: from |X_0|_F = 1 on, no singular value passes 1.2024, none of A 1.446, and b x + c x x stays in [-2.81, 0]
+// there.  That is what fp16 wants: they are stored times 2^14 (at most 46000), with 11 significant bits down to 4e-9.
 //   bf16 matrices with more than 384 rows and columns: factors rounded to fp16; X itself stays in 32 bits, and a X is added in 32 bits.  That matters:
 //     directions with singular values near zero are blown up by a per step, and so would be what rounding X puts
 //     there (a rounded X: 2e-2 of the result at 64 directions of 512; so: 7e-4, less than bf16 itself).  The result is
 //     1.02 to 1.5 times as far from 64 bits as its rounding to bf16 alone (the most with all singular values alike).
 //   fp32 matrices, and smaller bf16 ones (whose result one part leaves up to 2.8 times as far off, and whose products
-//   cost little): each factor as the sum of two fp16 parts, h = fp16(x), l = fp16(2^11 (x - h)), 22 bits and a sign;
-//     h l + l h, times 2^-11, + h h.  What is left out, l l, is below 2^-24 of the product of the elements: results
+//   cost little): each factor as the sum of two fp16 parts, h = fp16(x), l = fp16(x - h), 22 bits and a sign down to
+//     4e-6, an error of 2e-12 below;  h l + l h + h h.  What is left out, l l, is below 2^-24 of the product of the elements: results
 //     are as far from 64 bits as those of fp32 products (1.5e-6 at 512 x 512, both).
 #include "lc_operators.h"
 #include "lc_tile_product.h"
@@ -25,11 +25,10 @@ namespace lc {
 namespace {
 
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
-constexpr float kUp = 1024.f, kDown2 = 1.f / (1024.f * 1024.f);   // scale of stored factors, and of a product of two undone
-constexpr float kPart = 2048.f;                                   // scale of the second part
+constexpr float kUp = 16384.f, kDown2 = 1.f / (16384.f * 16384.f);   // scale of stored factors, and of a product of two undone
 constexpr int kOnePartSide = 384;   // see above
 constexpr int kBlock = 256;
-constexpr int kNormParts = 64;   // partial sums of squares of a replica at most
+constexpr int kNormParts = 1024;   // partial sums of squares of a replica at most
 
 enum OrthStep { kGram, kPoly, kNext, kLast };
 
@@ -73,7 +72,7 @@ struct Factors {
 __device__ __forceinline__ void split(float x, uint16_t& h, uint16_t& l) {
     const f16_t a = static_cast<f16_t>(x);
     h = __builtin_bit_cast(uint16_t, a);
-    l = __builtin_bit_cast(uint16_t, static_cast<f16_t>((x - static_cast<float>(a)) * kPart));
+    l = __builtin_bit_cast(uint16_t, static_cast<f16_t>(x - static_cast<float>(a)));
 }
 
 // M / |M| into X (32 bits and parts), 64 x 64 a workgroup, transposed where M is higher than wide.
@@ -85,7 +84,9 @@ __global__ void __launch_bounds__(kBlock) orth_start_kernel(OrthIn in, int n_par
     const T* src = static_cast<const T*>(in.src) + i * in.rep;
     const float* v = in.v ? in.v + i * in.v_rep : nullptr;
     if (threadIdx.x < 64) {
-        const double s = wave_sum(static_cast<int>(threadIdx.x) < n_parts ? in.parts[i * kNormParts + threadIdx.x] : 0.0);
+        double part = 0.0;
+        for (int k = threadIdx.x; k < n_parts; k += 64) part += in.parts[i * kNormParts + k];
+        const double s = wave_sum(part);
         // a zero matrix stays zero; a norm below what 1 / norm can be in 32 bits: as far as that goes
         if (threadIdx.x == 0) inv_s = s > 0.0 ? static_cast<float>(fmin(1.0 / sqrt(s), 3e38)) : s == 0.0 ? 0.f : static_cast<float>(s);
     }
@@ -147,7 +148,7 @@ __global__ void __launch_bounds__(S::kThreads) orth_product_kernel(TileArgs a, O
     const TilePlace pl = tile_place(a);
     if (pl.batch < 0) return;
     f32x4 acc[S::TM][S::TN];
-    tile_sums<f16_t, S, LB>(a, pl, 0, a.K / kTileK, lds, acc);
+    tile_sums<f16_t, S, LB>(a, pl, 0, a.K / S::BK, lds, acc);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int mw = pl.tm * S::BM + (w / S::WN) * S::TM * 16 + (lane & 15), nw = pl.tn * S::BN + (w % S::WN) * S::TN * 16 + (lane >> 4) * 4;
 #pragma unroll
@@ -213,9 +214,18 @@ __global__ void __launch_bounds__(S::kThreads) orth_product_kernel(TileArgs a, O
     }
 }
 
-typedef TileShape<256, 256, 2, 4, 2> Large;
-typedef TileShape<128, 128, 2, 2, 2> Medium;
-typedef TileShape<64, 64, 2, 2, 4> Small;
+template <int NP>
+struct Tiles {
+    typedef TileShape<256, 256, 2, 4, 64, 1, 2> Large;
+    typedef TileShape<128, 128, 2, 2, 64, 1, 2> Medium;
+    typedef TileShape<64, 64, 2, 2, 64, 1, 4> Small;
+};
+template <>
+struct Tiles<2> {
+    typedef TileShape<256, 256, 2, 4, 32, 2, 2> Large;
+    typedef TileShape<128, 128, 2, 2, 32, 2, 2> Medium;
+    typedef TileShape<64, 64, 2, 2, 64, 2, 4> Small;
+};
 
 template <typename S>
 void launch_product(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t st) {
@@ -231,14 +241,19 @@ void launch_product(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t st)
 }
 
 // Tile size: the largest that still gives most compute units a workgroup.
-void launch_step(const TileArgs& a, const OrthOut& o, OrthStep step, hipStream_t st) {
+template <int NP>
+void launch_step_parts(const TileArgs& a, const OrthOut& o, OrthStep step, hipStream_t st) {
     auto tiles = [&](int b) {
         const int64_t mt = (a.M + b - 1) / b, nt = (a.N + b - 1) / b;
         return (a.upper ? mt * (mt + 1) / 2 : mt * nt) * a.batches;
     };
-    if (tiles(256) >= 128) launch_product<Large>(a, o, step, st);
-    else if (tiles(128) >= 128) launch_product<Medium>(a, o, step, st);
-    else launch_product<Small>(a, o, step, st);
+    if (tiles(256) >= 128) launch_product<typename Tiles<NP>::Large>(a, o, step, st);
+    else if (tiles(128) >= 128) launch_product<typename Tiles<NP>::Medium>(a, o, step, st);
+    else launch_product<typename Tiles<NP>::Small>(a, o, step, st);
+}
+void launch_step(const TileArgs& a, const OrthOut& o, OrthStep step, int parts, hipStream_t st) {
+    if (parts == 2) launch_step_parts<2>(a, o, step, st);
+    else launch_step_parts<1>(a, o, step, st);
 }
 
 struct OrthPlan {
@@ -252,8 +267,8 @@ OrthPlan orth_plan(int m, int rows, int cols, int dtype, void* ws) {
     OrthPlan p;
     p.S = std::min(rows, cols);
     p.L = std::max(rows, cols);
-    p.Sp = static_cast<int>(round_up(p.S, kTileK));
-    p.Lp = static_cast<int>(round_up(p.L, kTileK));
+    p.Sp = static_cast<int>(round_up(p.S, kPadK));
+    p.Lp = static_cast<int>(round_up(p.L, kPadK));
     p.parts = dtype == LC_GEMM_BF16 && p.S > kOnePartSide ? 1 : 2;
     const int64_t nx = (int64_t)m * p.S * p.Lp, na = (int64_t)m * p.S * p.Sp;
     Carver c{static_cast<char*>(ws)};
@@ -271,7 +286,7 @@ OrthPlan orth_plan(int m, int rows, int cols, int dtype, void* ws) {
 // M (or the momentum that the step has just formed) through `steps` steps into o's place.
 int orthogonalise(int m, const OrthIn& in, int dtype, int steps, OrthOut o, const OrthPlan& p, hipStream_t st) {
     const bool bf16 = dtype == LC_GEMM_BF16;
-    const int tall = in.rows > in.cols, blocks = std::min(in.rows, kNormParts);
+    const int tall = in.rows > in.cols, blocks = std::min(in.rows, std::max(16, kNormParts / m));
     const int64_t nx = (int64_t)m * p.S * p.Lp, na = (int64_t)m * p.S * p.Sp;
     const dim3 gs(blocks, m), g0(p.Lp / 64, (p.S + 63) / 64, m);
     auto factors = [&](uint16_t* q, int64_t n) { return Factors{q, p.parts == 2 ? q + n : nullptr}; };
@@ -286,16 +301,10 @@ int orthogonalise(int m, const OrthIn& in, int dtype, int steps, OrthOut o, cons
     o.a = p.a; o.x = p.x;
     o.tall = tall;
     TileArgs t{};
-    t.segments = p.parts == 2 ? 3 : 1;
-    t.rescale_after = p.parts == 2 ? 2 : 0;
-    t.rescale = 1.f / kPart;
     t.batches = m;
     t.splits = 1;
-    // part offsets of the segments: h l, l h, h h
-    auto operand = [&](const uint16_t* q, int64_t n, int row, int64_t batch, int rows, int len, bool second) {
-        TileOperand r{q, row, batch, {}, rows, len};
-        if (p.parts == 2) r.part[second ? 0 : 1] = n;
-        return r;
+    auto operand = [&](const uint16_t* q, int64_t n, int row, int64_t batch, int rows, int len) {
+        return TileOperand{q, row, batch, {0, n, 0}, rows, len};
     };
     for (int k = 0; k < steps; ++k) {
         const uint16_t* x = p.xp[k & 1];
@@ -303,21 +312,21 @@ int orthogonalise(int m, const OrthIn& in, int dtype, int steps, OrthOut o, cons
         t.M = t.N = p.S;
         t.K = p.Lp;
         t.upper = 1;
-        t.a = operand(x, nx, p.Lp, bx, p.S, p.Lp, false);
-        t.b = operand(x, nx, p.Lp, bx, p.S, p.Lp, true);
+        t.a = operand(x, nx, p.Lp, bx, p.S, p.Lp);
+        t.b = operand(x, nx, p.Lp, bx, p.S, p.Lp);
         o.to = factors(p.ap, na);
-        launch_step(t, o, kGram, st);
+        launch_step(t, o, kGram, p.parts, st);
         t.K = p.Sp;
-        t.a = operand(p.ap, na, p.Sp, ba, p.S, p.Sp, false);
-        t.b = operand(p.ap, na, p.Sp, ba, p.S, p.Sp, true);
+        t.a = operand(p.ap, na, p.Sp, ba, p.S, p.Sp);
+        t.b = operand(p.ap, na, p.Sp, ba, p.S, p.Sp);
         o.to = factors(p.bp, na);
-        launch_step(t, o, kPoly, st);
+        launch_step(t, o, kPoly, p.parts, st);
         t.upper = 0;
         t.N = p.Lp;
-        t.a = operand(p.bp, na, p.Sp, ba, p.S, p.Sp, false);
-        t.b = operand(x, nx, p.Lp, bx, p.S, p.Lp, true);   // S rows of k
+        t.a = operand(p.bp, na, p.Sp, ba, p.S, p.Sp);
+        t.b = operand(x, nx, p.Lp, bx, p.S, p.Lp);   // S rows of k
         o.to = factors(p.xp[(k + 1) & 1], nx);
-        launch_step(t, o, k + 1 < steps ? kNext : kLast, st);
+        launch_step(t, o, k + 1 < steps ? kNext : kLast, p.parts, st);
     }
     return hipGetLastError() == hipSuccess ? LC_OK : LC_ERR_HIP;
 }

@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, Lo
     const int kept = __builtin_amdgcn_readfirstlane(l.kept[pl.batch]) - l.base;
     if (pl.tm * S::BM >= kept) return;
     f32x4 acc[S::TM][S::TN];
-    tile_sums<bf16_t, S, NMajor>(a, pl, 0, a.K / kTileK, lds, acc);
+    tile_sums<bf16_t, S, NMajor>(a, pl, 0, a.K / S::BK, lds, acc);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w / S::WN, wn = w % S::WN;
     const int nw = pl.tn * S::BN + wn * S::TN * 16 + (lane >> 4) * 4;
     const float* bias = l.bias ? l.bias + pl.batch * l.bias_rep : nullptr;
@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(S::kThreads) head_da_kernel(TileArgs a, float*
     const TilePlace pl = tile_place(a);
     if (pl.batch < 0) return;
     int k0, k1;
-    tile_k_range(a, pl, S::BM, k0, k1);
+    tile_k_range<S>(a, pl, k0, k1);
     if (a.m_count && pl.tm * S::BM >= __builtin_amdgcn_readfirstlane(a.m_count[pl.batch]) - a.count_base) return;
     f32x4 acc[S::TM][S::TN];
     tile_sums<bf16_t, S, KMajor>(a, pl, k0, k1, lds, acc);
@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across
     const TilePlace pl = tile_place(a);
     if (pl.batch < 0) return;
     int k0, k1;
-    tile_k_range(a, pl, S::BM, k0, k1);
+    tile_k_range<S>(a, pl, k0, k1);
     f32x4 acc[S::TM][S::TN];
     tile_sums<bf16_t, S, NMajor>(a, pl, k0, k1, lds, acc);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -489,12 +489,22 @@ __global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across
 
 // ------------------------------------------------------------------ host
 
-typedef TileShape<64, 256, 1, 4, 2> Rows64;
-typedef TileShape<128, 256, 2, 4, 3> Rows128;
-typedef TileShape<256, 256, 2, 4, 2> Rows256;
+// Tiles of the products: one part (bf16 operands) or three (fp32).
+template <bool THREE>
+struct Tiles {
+    typedef TileShape<64, 256, 1, 4, 64, 1, 2> Rows64;
+    typedef TileShape<128, 256, 2, 4, 64, 1, 3> Rows128;
+    typedef TileShape<256, 256, 2, 4, 64, 1, 2> Rows256;
+};
+template <>
+struct Tiles<true> {
+    typedef TileShape<64, 256, 1, 4, 32, 3, 2> Rows64;
+    typedef TileShape<128, 256, 2, 4, 32, 3, 2> Rows128;
+    typedef Rows128 Rows256;   // 256 x 256 in three parts would take 192 KB of LDS for two buffers
+};
 
 // A product's tile by its rows: no taller than they need, 256 where there are more.
-template <typename F>
+template <bool THREE, typename F>
 void with_tile(TileArgs& a, F f) {
     auto go = [&](auto shape) {
         typedef decltype(shape) S;
@@ -502,9 +512,9 @@ void with_tile(TileArgs& a, F f) {
         a.nt = (a.N + S::BN - 1) / S::BN;
         f(shape);
     };
-    if (a.M <= 64) go(Rows64());
-    else if (a.M <= 128) go(Rows128());
-    else go(Rows256());
+    if (a.M <= 64) go(typename Tiles<THREE>::Rows64());
+    else if (a.M <= 128) go(typename Tiles<THREE>::Rows128());
+    else go(typename Tiles<THREE>::Rows256());
 }
 
 struct HeadPlan {
@@ -549,9 +559,9 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
     p.grad = grad;
     p.three = h.dtype == LC_GEMM_FP32;
     p.d = h.inputs;
-    p.dp = static_cast<int>(round_up(h.inputs, kTileK));
+    p.dp = static_cast<int>(round_up(h.inputs, kPadK));
     p.parts = static_cast<int>((h.classes + kWide - 1) / kWide);
-    p.ep = round_up(h.classes, kTileK);
+    p.ep = round_up(h.classes, kPadK);
     // bf16 weights are read where they stand if every row starts on 16 bytes and holds whole chunks of 8
     p.copy_w = p.three || h.classes % 8 || !aligned_to(h.W.p, 16) || (h.inputs > 1 && h.W.row % 8) || (h.m > 1 && h.W.replica % 8) ||
                h.W.row > kMaxRowStride;
@@ -579,9 +589,11 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
         t.M = static_cast<int>(n);
         t.N = p.d;
         int64_t tiles = 1;
-        with_tile(t, [&](auto) { tiles = (int64_t)t.mt * t.nt * g; });
+        auto count = [&](auto) { tiles = (int64_t)t.mt * t.nt * g; };
+        if (p.three) with_tile<true>(t, count);
+        else with_tile<false>(t, count);
         // few tiles: the classes are shared out until every compute unit has a share, of 8 tiles of k at least
-        p.splits = static_cast<int>(std::max<int64_t>(1, std::min((256 + tiles - 1) / tiles, p.ep / (8 * kTileK))));
+        p.splits = static_cast<int>(std::max<int64_t>(1, std::min((256 + tiles - 1) / tiles, p.ep / (8 * kPadK))));
         p.coef = c.take<float>(g * n * p.parts);
         p.delta_label = c.take<float>(g * n);
         p.at = c.take<uint16_t>(np * g * p.d * n);
@@ -596,13 +608,11 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
     return p;
 }
 
-// The six part products of two fp32 operands, smallest first; parts `pa` and `pb` elements apart.
-void segments(TileArgs& t, bool three, int64_t pa, int64_t pb) {
-    static const int ia[6] = {0, 1, 2, 0, 1, 0}, ib[6] = {2, 1, 0, 1, 0, 0};
-    t.segments = three ? 6 : 1;
-    for (int s = 0; s < t.segments && three; ++s) {
-        t.a.part[s] = ia[s] * pa;
-        t.b.part[s] = ib[s] * pb;
+// Where the parts of two operands stand.
+void set_parts(TileArgs& t, int64_t pa, int64_t pb) {
+    for (int p = 0; p < kMaxParts; ++p) {
+        t.a.part[p] = p * pa;
+        t.b.part[p] = p * pb;
     }
 }
 
@@ -634,7 +644,7 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             TileArgs t{};
             t.a = TileOperand{p.a, p.dp, n * p.dp, {}, here, p.dp};
             t.b = w;
-            segments(t, p.three, a_part, w_part);
+            set_parts(t, a_part, w_part);
             t.M = here;
             t.N = h.classes;
             t.K = p.dp;
@@ -644,7 +654,7 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
                               h.classes, p.parts, p.stat, p.z_label, p.grad ? (p.three ? (void*)p.e32 : (void*)p.dz) : nullptr, p.ep};
             typedef typename std::conditional<sizeof(T) == 4, float, f16_t>::type E;
             if (here) {
-                with_tile(t, [&](auto s) {
+                with_tile<sizeof(T) == 4>(t, [&](auto s) {
                     typedef decltype(s) S;
                     head_logits_kernel<S, E><<<tile_grid(t), S::kThreads, 0, st>>>(t, l);
                 });
@@ -664,7 +674,7 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             t = TileArgs{};
             t.a = TileOperand{p.dz, p.ep, n * p.ep, {}, here, static_cast<int>(p.ep)};
             t.b = w;
-            segments(t, p.three, dz_part, w_part);
+            set_parts(t, dz_part, w_part);
             t.M = here;
             t.N = p.d;
             t.K = static_cast<int>(p.ep);
@@ -673,7 +683,7 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             t.m_count = kept;
             t.count_base = base;
             if (here) {
-                with_tile(t, [&](auto s) {
+                with_tile<sizeof(T) == 4>(t, [&](auto s) {
                     typedef decltype(s) S;
                     head_da_kernel<S><<<tile_grid(t), S::kThreads, 0, st>>>(t, p.da, static_cast<int>(n), p.d);
                 });
@@ -684,10 +694,10 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             t = TileArgs{};
             t.a = TileOperand{p.at, n, p.d * n, {}, p.d, static_cast<int>(n)};
             t.b = TileOperand{p.dz, p.ep, n * p.ep, {}, static_cast<int>(n), static_cast<int>(p.ep)};
-            segments(t, p.three, at_part, dz_part);
+            set_parts(t, at_part, dz_part);
             t.M = p.d;
             t.N = h.classes;
-            t.K = static_cast<int>(round_up(here, kTileK));
+            t.K = static_cast<int>(round_up(here, kPadK));
             t.batches = g;
             t.splits = 1;
             t.k_count = kept;
@@ -696,7 +706,7 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             G* dW = static_cast<G*>(h.dW.p) + g0 * h.dW.replica;
             const size_t gb = 4 * sizeof(G);
             const int vec = aligned_to(dW, gb) && h.dW.row % 4 == 0 && (h.m == 1 || h.dW.replica % 4 == 0);
-            with_tile(t, [&](auto s) {
+            with_tile<sizeof(T) == 4>(t, [&](auto s) {
                 typedef decltype(s) S;
                 head_dw_kernel<S, G><<<tile_grid(t), S::kThreads, 0, st>>>(t, x, dW, h.dW.row, h.dW.replica, vec);
             });

@@ -1,17 +1,22 @@
 // Tiled products of 16-bit operands with 32-bit sums: the core of the softmax head and of the
 // Newton-Schulz products.  Internal linkage: every translation unit gets its own copy.
 //
-//   acc[m, n] = sum over segments s, k of A_s[m, k] B_s[k, n]
+//   acc[m, n] = sum_k A[m, k] B[k, n]
 //
 // A stands with k contiguous; B with k contiguous (KMajor: rows n) or with n contiguous (NMajor: rows
-// k, read through the LDS transpose).  A segment is one pair of parts: fp32 operands come as the sum of
-// 16-bit parts, and a product of two such sums is a list of part products over one accumulator.
+// k, read through the LDS transpose).  A 32-bit operand comes as the sum of NP 16-bit parts, and its product
+// as those of the parts that matter: two parts 0 1 + 1 0 + 0 0, three 0 2 + 1 1 + 2 0 + 0 1 + 1 0 + 0 0, all from one
+// stay of the parts' tiles in LDS.
 //
-// A workgroup owns a BM x BN tile.  Tiles of 64 k of both operands go from global memory straight into
+// A workgroup owns a BM x BN tile.  Tiles of BK k of both operands go from global memory straight into
 // LDS (16 bytes a lane, no registers), into two to four buffers in turn.  16-byte chunks are permuted inside a row,
 // by permuting what each lane fetches, so that the operand reads of a wavefront spread over all banks:
-//   KMajor  row of 64 k = 8 chunks:    chunk c of row r at c ^ ((r >> 1) & 7)
+//   KMajor  row of 64 k = 8 chunks:    chunk c of row r at c ^ ((r >> 1) & 7);  of 32 k: at c ^ ((r >> 2) & 3)
 //   NMajor  row of BN n, 32-byte pairs: pair p of row k at p ^ ((k & 3) | (k >> 3 & 1) << 2), as far as there are pairs
+//
+// What bounds it: 64 KB of operands a k tile of 64 come out of the caches at about 10 TB/s over the chip (8192^3, where
+// 8 x 4 tiles of an XCD share them: 0.9 ms alone), LDS reads and the matrix cores could do 0.5 and 0.7 ms: 1.16 ms
+// together, 945 TFLOP/s.  Tiles of 32 k in four buffers: 844.
 #pragma once
 #include "lc_internal.h"
 
@@ -24,8 +29,8 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kTileK = 64;
-constexpr int kMaxSegments = 6;
+constexpr int kPadK = 64;      // what the callers pad k to
+constexpr int kMaxParts = 3;
 
 __device__ __forceinline__ f32x4 mma32(bf16_t, s16x8 a, s16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -40,7 +45,7 @@ __device__ __forceinline__ f32x4 mma32(f16_t, s16x8 a, s16x8 b, f32x4 c) {
 struct TileOperand {
     const uint16_t* p;
     int64_t row, batch;
-    int64_t part[kMaxSegments];   // offset of the part that a segment takes
+    int64_t part[kMaxParts];      // where its parts stand
     int rows, len;                // KMajor: rows of k, `len` of them; NMajor: `rows` k of `len` n.  len % 8 == 0,
                                   // the k padded to 64 are those of the product
 };
@@ -49,9 +54,6 @@ constexpr int64_t kMaxRowStride = 1 << 22;   // offsets inside a tile of 256 row
 struct TileArgs {
     TileOperand a, b;
     int M, N, K;                  // K: padded to 64, A is zero behind its own length
-    int segments;
-    int rescale_after;            // the sums are multiplied by `rescale` before this segment (0: never)
-    float rescale;
     int batches, mt, nt, splits;  // tiles in M and N, shares of the K axis
     int upper;                    // symmetric result: only tiles with tm <= tn, (mt (mt + 1) / 2 of them)
     const int* m_count;           // [batches] rows of A that count, or null; tiles behind them run no product
@@ -61,15 +63,18 @@ struct TileArgs {
 
 enum BLayout { KMajor, NMajor };
 
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+template <int BM_, int BN_, int WM_, int WN_, int BK_, int NP_, int STAGES_>
 struct TileShape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;   // WM x WN wavefronts
+    static constexpr int BK = BK_, NP = NP_, KS = BK / 32;
     static constexpr int kThreads = 64 * WM * WN;
     static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;     // 16 x 16 tiles of a wavefront
-    static constexpr int kStage = (BM + BN) * kTileK;              // elements of one LDS buffer
+    static constexpr int kPart = (BM + BN) * BK;                   // elements of one part's tiles: A's, then B's
+    static constexpr int kStage = NP * kPart;                      // ... of one LDS buffer
     static constexpr int kStages = STAGES_, kLds = kStages * kStage;
     static constexpr int kLoads = kStage / 8 / kThreads;           // load instructions of a thread for a buffer
-    static_assert(kStage % (8 * kThreads) == 0 && kLoads * (kStages - 2) < 64, "what a wait can count");
+    static_assert(kPart % (8 * kThreads) == 0 && kLoads * (kStages - 2) < 64, "what a wait can count");
+    static_assert(BM * BK % (8 * kThreads) == 0 && kLds * 2 <= 160 * 1024 && TM % 2 == 0 && TN % 2 == 0, "");
 };
 
 typedef __attribute__((address_space(3))) void* LdsPtr;
@@ -82,37 +87,37 @@ __device__ __forceinline__ void fetch16(const char* base, uint32_t off, uint16_t
 
 // What a lane fetches of R rows of a KMajor operand: offsets (bytes) from the tile's first row and column; `base` of
 // fetch() is the tile's first row.
-template <int R, int THREADS>
+template <int R, int BK, int THREADS>
 struct KMajorFetch {
-    static constexpr int kPer = THREADS / 8, kLoads = R / kPer;   // rows per load instruction of the workgroup
+    static constexpr int kChunks = BK / 8, kPer = THREADS / kChunks, kLoads = R / kPer;   // rows per load instruction of the workgroup
     uint32_t off[kLoads];
     int c8;   // the lane's first k inside a tile
     __device__ __forceinline__ void init(const TileOperand& o, int row0) {
         const int t = threadIdx.x;
         static_assert(kPer % 16 == 0, "the permutation of a lane's chunk is the same in all its rows");
-        c8 = ((t & 7) ^ ((t >> 4) & 7)) * 8;
+        c8 = (BK == 64 ? (t & 7) ^ ((t >> 4) & 7) : (t & 3) ^ ((t >> 4) & 3)) * 8;
 #pragma unroll
         for (int q = 0; q < kLoads; ++q)
-            off[q] = ((uint32_t)(min(row0 + q * kPer + (t >> 3), o.rows - 1) - row0) * (uint32_t)o.row + c8) * 2u;
+            off[q] = ((uint32_t)(min(row0 + q * kPer + t / kChunks, o.rows - 1) - row0) * (uint32_t)o.row + c8) * 2u;
     }
     __device__ __forceinline__ void fetch(const TileOperand& o, const char* base, int k0, uint16_t* to) const {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        to += wave * 8 * kTileK;
+        to += wave * 512;
         const char* at = base + 2 * (int64_t)k0;
-        if (k0 + kTileK <= o.len) {
+        if (k0 + BK <= o.len) {
 #pragma unroll
-            for (int q = 0; q < kLoads; ++q) fetch16(at, off[q], to + q * kPer * kTileK);
+            for (int q = 0; q < kLoads; ++q) fetch16(at, off[q], to + q * THREADS * 8);
         } else {
             const int k = min(k0 + c8, o.len - 8);
 #pragma unroll
-            for (int q = 0; q < kLoads; ++q) fetch16(base, off[q] + 2u * (uint32_t)(k - c8), to + q * kPer * kTileK);
+            for (int q = 0; q < kLoads; ++q) fetch16(base, off[q] + 2u * (uint32_t)(k - c8), to + q * THREADS * 8);
         }
     }
 };
 // ... of BN columns of an NMajor operand: offsets from the k tile's first row.
-template <int BN, int THREADS>
+template <int BN, int BK, int THREADS>
 struct NMajorFetch {
-    static constexpr int kChunks = BN / 8, kPer = THREADS / kChunks, kLoads = kTileK / kPer;
+    static constexpr int kChunks = BN / 8, kPer = THREADS / kChunks, kLoads = BK / kPer;
     uint32_t col;   // bytes
     int k;
     uint32_t row2;  // bytes of a row
@@ -132,7 +137,7 @@ struct NMajorFetch {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         to += wave * 512;
         const char* at = base + (int64_t)k0 * row2;
-        if (k0 + kTileK <= o.rows) {
+        if (k0 + BK <= o.rows) {
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) fetch16(at, off[q], to + q * THREADS * 8);
         } else {
@@ -147,9 +152,10 @@ struct NMajorFetch {
     }
 };
 
+template <int BK>
 __device__ __forceinline__ s16x8 read_kmajor(const uint16_t* tile, int row, int ks, int lane) {
-    const int c = (ks * 4 + (lane >> 4)) ^ ((lane >> 1) & 7);
-    return *reinterpret_cast<const s16x8*>(tile + (row + (lane & 15)) * kTileK + c * 8);
+    const int c = BK == 64 ? (ks * 4 + (lane >> 4)) ^ ((lane >> 1) & 7) : (lane >> 4) ^ ((lane >> 2) & 3);
+    return *reinterpret_cast<const s16x8*>(tile + (row + (lane & 15)) * BK + c * 8);
 }
 // A 16-lane group reads 4 rows of k, 16 columns; lane i gets column i of all four.
 template <int BN>
@@ -164,13 +170,13 @@ __device__ __forceinline__ s16x8 read_nmajor(const uint16_t* tile, int col, int 
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-template <BLayout L, int BN, int THREADS>
+template <BLayout L, typename S>
 struct FetchB {
-    typedef KMajorFetch<BN, THREADS> type;
+    typedef KMajorFetch<S::BN, S::BK, S::kThreads> type;
 };
-template <int BN, int THREADS>
-struct FetchB<NMajor, BN, THREADS> {
-    typedef NMajorFetch<BN, THREADS> type;
+template <typename S>
+struct FetchB<NMajor, S> {
+    typedef NMajorFetch<S::BN, S::BK, S::kThreads> type;
 };
 
 struct TilePlace {
@@ -232,8 +238,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
                                           f32x4 (&acc)[S::TM][S::TN]) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WN, wn = wave % S::WN;
-    const int m0 = pl.tm * S::BM, n0 = pl.tn * S::BN;
-    const int per_seg = kt1 - kt0, total = per_seg * a.segments;
+    const int m0 = pl.tm * S::BM, n0 = pl.tn * S::BN, total = kt1 - kt0;
 #pragma unroll
     for (int i = 0; i < S::TM; ++i)
 #pragma unroll
@@ -241,53 +246,65 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
     if (total <= 0) return;
     const char* ab = reinterpret_cast<const char*>(a.a.p + (int64_t)pl.batch * a.a.batch + (int64_t)m0 * a.a.row);
     const char* bb = reinterpret_cast<const char*>(a.b.p + (int64_t)pl.batch * a.b.batch + (L == KMajor ? (int64_t)n0 * a.b.row : 0));
-    KMajorFetch<S::BM, S::kThreads> fetch_a;
-    typename FetchB<L, S::BN, S::kThreads>::type fetch_b;
+    KMajorFetch<S::BM, S::BK, S::kThreads> fetch_a;
+    typename FetchB<L, S>::type fetch_b;
     fetch_a.init(a.a, m0);
     fetch_b.init(a.b, n0);
-    constexpr int NS = S::kStages;
-    int seg = 0, next_k = kt0, next_buf = 0;   // of the tile that is fetched next
-    auto ask_a = [&] { fetch_a.fetch(a.a, ab + 2 * a.a.part[seg], next_k * kTileK, lds + next_buf * S::kStage); };
+    constexpr int NS = S::kStages, NP = S::NP, KS = S::KS;
+    int next_k = kt0 * S::BK, next_buf = 0;   // of the tile that is fetched next
+    auto ask_a = [&] {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) fetch_a.fetch(a.a, ab + 2 * a.a.part[p], next_k, lds + next_buf * S::kStage + p * S::kPart);
+    };
     auto ask_b = [&] {
-        fetch_b.fetch(a.b, bb + 2 * a.b.part[seg], next_k * kTileK, lds + next_buf * S::kStage + S::BM * kTileK);
-        if (++next_k == kt1) next_k = kt0, ++seg;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+            fetch_b.fetch(a.b, bb + 2 * a.b.part[p], next_k, lds + next_buf * S::kStage + p * S::kPart + S::BM * S::BK);
+        next_k += S::BK;
         next_buf = next_buf + 1 == NS ? 0 : next_buf + 1;
     };
-    const int rescale_at = a.rescale_after ? a.rescale_after * per_seg : -1;
     const int ahead = min(NS - 1, total);
     for (int t = 0; t < ahead; ++t) {
         ask_a();
         ask_b();
     }
     int buf = 0;
-    // a quarter of the wavefront's tile at a time: half of its rows by half of its columns, both 32-deep steps
+    // a quarter of the wavefront's tile at a time: half of its rows by half of its columns, all parts and 32-deep steps
     constexpr int HM = S::TM / 2, HN = S::TN / 2;
-    s16x8 fa[HM][2], fb[2][HN][2];
+    s16x8 fa[HM][NP][KS], fb[2][HN][NP][KS];
     auto read_b = [&](const uint16_t* tb, int h) {
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+        for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int j = 0; j < HN; ++j) {
-                if constexpr (L == KMajor)
-                    fb[h][j][ks] = read_kmajor(tb, (wn * S::TN + h * HN + j) * 16, ks, lane);
-                else
-                    fb[h][j][ks] = read_nmajor<S::BN>(tb, (wn * S::TN + h * HN + j) * 16, ks, lane);
-            }
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int j = 0; j < HN; ++j) {
+                    if constexpr (L == KMajor)
+                        fb[h][j][p][ks] = read_kmajor<S::BK>(tb + p * S::kPart, (wn * S::TN + h * HN + j) * 16, ks, lane);
+                    else
+                        fb[h][j][p][ks] = read_nmajor<S::BN>(tb + p * S::kPart, (wn * S::TN + h * HN + j) * 16, ks, lane);
+                }
     };
     auto read_a = [&](const uint16_t* ta, int h) {
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+        for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int i = 0; i < HM; ++i) fa[i][ks] = read_kmajor(ta, (wm * S::TM + h * HM + i) * 16, ks, lane);
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int i = 0; i < HM; ++i) fa[i][p][ks] = read_kmajor<S::BK>(ta + p * S::kPart, (wm * S::TM + h * HM + i) * 16, ks, lane);
     };
     auto mma = [&](int hm, int hn) {
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-            for (int i = 0; i < HM; ++i)
+            for (int sum = NP - 1; sum >= 0; --sum)   // the smallest part products first
 #pragma unroll
-                for (int j = 0; j < HN; ++j)
-                    acc[hm * HM + i][hn * HN + j] = mma32(T(), fb[hn][j][ks], fa[i][ks], acc[hm * HM + i][hn * HN + j]);
+                for (int p = 0; p <= sum; ++p)
+#pragma unroll
+                    for (int i = 0; i < HM; ++i)
+#pragma unroll
+                        for (int j = 0; j < HN; ++j)
+                            acc[hm * HM + i][hn * HN + j] = mma32(T(), fb[hn][j][sum - p][ks], fa[i][p][ks], acc[hm * HM + i][hn * HN + j]);
     };
     auto turn = [&](int hm, int hn) {   // operands are there: this half's turn at the matrix cores
         __builtin_amdgcn_s_waitcnt(kWaitLds);
@@ -296,12 +313,6 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         mma(hm, hn);
         __builtin_amdgcn_s_setprio(0);
         tile_barrier();
-    };
-    auto rescale = [&] {
-#pragma unroll
-        for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-            for (int j = 0; j < S::TN; ++j) acc[i][j] *= a.rescale;
     };
     auto oldest = [&](int asked) {   // tiles asked for beyond the one that is waited for
         if (asked == NS - 2) __builtin_amdgcn_s_waitcnt(wait_loads((NS - 2) * S::kLoads));
@@ -313,10 +324,9 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         tile_barrier();
         if (late) tile_barrier();
         for (int t = 0; t < total; ++t) {
-            const uint16_t *ta = lds + buf * S::kStage, *tb = ta + S::BM * kTileK;
+            const uint16_t *ta = lds + buf * S::kStage, *tb = ta + S::BM * S::BK;
             buf = buf + 1 == NS ? 0 : buf + 1;
             const bool more = t + NS - 1 < total;
-            if (t == rescale_at) rescale();
             read_b(tb, 0);
             read_a(ta, 0);
             if (more) ask_a();
@@ -334,13 +344,12 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         for (int t = 0; t < total; ++t) {
             oldest(min(total - t, NS - 1) - 1);
             tile_barrier();   // the tile is there, and all have read the one whose place is filled next
-            const uint16_t *ta = lds + buf * S::kStage, *tb = ta + S::BM * kTileK;
+            const uint16_t *ta = lds + buf * S::kStage, *tb = ta + S::BM * S::BK;
             buf = buf + 1 == NS ? 0 : buf + 1;
             if (t + NS - 1 < total) {
                 ask_a();
                 ask_b();
             }
-            if (t == rescale_at) rescale();
             read_b(tb, 0);
             read_a(ta, 0);
             read_b(tb, 1);
@@ -356,11 +365,12 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
 }
 
 // The k tiles [kt0, kt1) of a workgroup's share.
-__device__ __forceinline__ void tile_k_range(const TileArgs& a, const TilePlace pl, int bm, int& kt0, int& kt1) {
-    int kt = a.K / kTileK;
+template <typename S>
+__device__ __forceinline__ void tile_k_range(const TileArgs& a, const TilePlace pl, int& kt0, int& kt1) {
+    int kt = a.K / S::BK;
     if (a.k_count)
-        kt = min(kt, (max(0, __builtin_amdgcn_readfirstlane(a.k_count[pl.batch]) - a.count_base) + kTileK - 1) / kTileK);
-    if (a.m_count && pl.tm * bm >= __builtin_amdgcn_readfirstlane(a.m_count[pl.batch]) - a.count_base) kt = 0;
+        kt = min(kt, (max(0, __builtin_amdgcn_readfirstlane(a.k_count[pl.batch]) - a.count_base) + S::BK - 1) / S::BK);
+    if (a.m_count && pl.tm * S::BM >= __builtin_amdgcn_readfirstlane(a.m_count[pl.batch]) - a.count_base) kt = 0;
     kt0 = (int)((int64_t)kt * pl.split / a.splits);
     kt1 = (int)((int64_t)kt * (pl.split + 1) / a.splits);
 }
