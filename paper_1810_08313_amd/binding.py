@@ -273,191 +273,223 @@ def adacomm_next_tau_ex(F0: float, Fl: float, tau0: int, tau_prev: int, gamma: f
 # current one); results may be given instead: `out`, `dx`, ... of the same shape.  The last axis is contiguous, the
 # other two have any distances, so that a layer's place in the rows of X or G will do.
 
-ERR_ARG, ERR_ALIGN = -1, -4
+ERR_ARG = -1
 
 
-def _need(ok: bool, where: str, what: str) -> None:
-    if not ok:
-        e = LcError(ERR_ARG, where)
-        e.args = (f"{where}: {what} ({ERR_ARG})",)
-        raise e
+def _refuse(where: str, what: str) -> None:
+    e = LcError(ERR_ARG, where)
+    e.args = (f"{where}: {what} ({ERR_ARG})",)
+    raise e
 
 
-class _Call:
-    """The stream, device and element type that a call's tensors share; checks them."""
-
-    def __init__(self, where: str, first, dtypes, stream):
-        import torch
-        self.torch, self.where, self.device = torch, where, first.device
-        _need(first.is_cuda, where, "tensors of a GPU are needed")
-        _need(first.dtype in dtypes, where, f"element type {first.dtype}")
-        self.stream = stream if stream is not None else torch.cuda.current_stream(first.device)
-        _need(self.stream.device == first.device, where, "the stream is another device's")
-
-    def code(self, dtype) -> int:
-        return GEMM_BF16 if dtype == self.torch.bfloat16 else GEMM_FP32
-
-    def check(self, t, name, shape, dtype) -> None:
-        _need(t.device == self.device, self.where, f"{name} is on {t.device}, not on {self.device}")
-        _need(t.dtype == dtype, self.where, f"{name} has element type {t.dtype}, not {dtype}")
-        _need(tuple(t.shape) == tuple(shape), self.where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-        _need(t.numel() == 0 or t.shape[-1] == 1 or t.stride(-1) == 1, self.where, f"{name}: the last axis is not contiguous")
-
-    def rows(self, t, name, shape, dtype) -> LcRows:
-        self.check(t, name, shape, dtype)
-        return LcRows(t.data_ptr(), t.stride(1), t.stride(0))
-
-    def vector(self, t, name, shape, dtype):
-        """(pointer, distance of replicas) of a [m, n] tensor, or of None."""
-        if t is None:
-            return None, 0
-        self.check(t, name, shape, dtype)
-        return t.data_ptr(), t.stride(0)
-
-    def run(self, fn):
-        """fn() on the call's device, what it allocates belonging to the call's stream."""
-        if self.torch.cuda.current_device() == self.device.index and self.torch.cuda.current_stream(self.device) == self.stream:
-            return fn()
-        with self.torch.cuda.device(self.device), self.torch.cuda.stream(self.stream):
-            return fn()
-
-    def workspace(self, n: int):
-        return self.torch.empty(max(int(n), 1), dtype=self.torch.uint8, device=self.device)
-
-    def status(self, rc: int) -> None:
-        if rc != 0:
-            raise LcError(rc, self.where)
+def _first(where: str, t, stream):
+    """The stream of a call, from its first tensor [m, rows, cols], and whether it is not what torch's allocator would
+    take by itself."""
+    import torch
+    if not t.is_cuda:
+        _refuse(where, "tensors of a GPU are needed")
+    if t.dim() != 3:
+        _refuse(where, f"a tensor of shape {tuple(t.shape)} where [m, rows, cols] is needed")
+    if t.dtype is not torch.float32 and t.dtype is not torch.bfloat16:
+        _refuse(where, f"element type {t.dtype}")
+    here = torch.cuda.current_device() == t.get_device()
+    if stream is None:
+        return torch.cuda.current_stream(t.device), not here
+    if stream.device != t.device:
+        _refuse(where, "the stream is another device's")
+    return stream, not here or stream != torch.cuda.current_stream(t.device)
 
 
-def _types(torch):
-    return (torch.float32, torch.bfloat16)
+def _on(stream):
+    """Context in which what is allocated belongs to the stream that the call runs on."""
+    import torch
+    return torch.cuda.stream(stream)   # of its device, too
+
+
+def _check(where: str, name: str, t, shape, dtype, device) -> tuple:
+    """The tensor's strides."""
+    st = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.device != device or (st[-1] != 1 and shape[-1] > 1 and t.numel()):
+        if t.device != device:
+            _refuse(where, f"{name} is on {t.device}, not on {device}")
+        if t.dtype is not dtype:
+            _refuse(where, f"{name} has element type {t.dtype}, not {dtype}")
+        if t.shape != shape:
+            _refuse(where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+        _refuse(where, f"{name}: the last axis is not contiguous")
+    return st
+
+
+def _rows(where, name, t, shape, dtype, device) -> LcRows:
+    st = _check(where, name, t, shape, dtype, device)
+    return LcRows(t.data_ptr(), st[1], st[0])
+
+
+def _vector(where, name, t, shape, dtype, device):
+    """(pointer, distance of replicas) of a [m, n] tensor, or of None."""
+    if t is None:
+        return None, 0
+    return t.data_ptr(), _check(where, name, t, shape, dtype, device)[0]
+
+
+def _workspace(n: int, device):
+    import torch
+    return torch.empty(n or 1, dtype=torch.uint8, device=device)
 
 
 def layer_norm(x, gain=None, bias=None, eps: float = 1e-5, out=None, stream=None):
     """lc_layer_norm on x [m, rows, cols] (fp32 or bfloat16), gain and bias fp32 [m, cols] or None.
     Returns y and the statistics [m, rows, 2] that layer_norm_grad takes."""
     import torch
-    c = _Call("lc_layer_norm", x, _types(torch), stream)
-    _need(x.dim() == 3, c.where, "x is [m, rows, cols]")
-    m, rows, cols = x.shape
-
-    def go():
-        y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
-        stats = torch.empty((m, rows, 2), dtype=torch.float32, device=x.device)
-        (gp, gs), (bp, bs) = c.vector(gain, "gain", (m, cols), torch.float32), c.vector(bias, "bias", (m, cols), torch.float32)
-        _need(gain is None or bias is None or gs == bs, c.where, "gain and bias have different distances between replicas")
-        c.status(lib().lc_layer_norm(m, rows, cols, c.code(x.dtype), c.rows(x, "x", x.shape, x.dtype), gp, bp, gs or bs, eps,
-                                     c.rows(y, "out", x.shape, x.dtype), stats.data_ptr(), c.stream.cuda_stream))
-        return y, stats
-    return c.run(go)
+    where = "lc_layer_norm"
+    stream, other = _first(where, x, stream)
+    if other:
+        with _on(stream):
+            return layer_norm(x, gain, bias, eps, out)
+    f32, t, dev, shape = torch.float32, x.dtype, x.device, x.shape
+    m, rows, cols = shape
+    y = torch.empty(shape, dtype=t, device=dev) if out is None else out
+    stats = torch.empty((m, rows, 2), dtype=f32, device=dev)
+    gp, gs = _vector(where, "gain", gain, (m, cols), f32, dev)
+    bp, bs = _vector(where, "bias", bias, (m, cols), f32, dev)
+    if gs != bs and gp and bp and m > 1:
+        _refuse(where, "gain and bias have different distances between replicas")
+    rc = lib().lc_layer_norm(m, rows, cols, t is torch.bfloat16, _rows(where, "x", x, shape, t, dev), gp, bp, gs or bs, eps,
+                             _rows(where, "out", y, shape, t, dev), stats.data_ptr(), stream.cuda_stream)
+    if rc:
+        raise LcError(rc, where)
+    return y, stats
 
 
 def layer_norm_grad(x, dy, gain, stats, dx=None, dgain=None, dbias=None, stream=None):
     """lc_layer_norm_grad: dx, dgain and dbias (fp32 [m, cols]) from dy and what layer_norm returned."""
     import torch
-    c = _Call("lc_layer_norm_grad", x, _types(torch), stream)
-    _need(x.dim() == 3, c.where, "x is [m, rows, cols]")
-    m, rows, cols = x.shape
+    where = "lc_layer_norm_grad"
+    stream, other = _first(where, x, stream)
+    if other:
+        with _on(stream):
+            return layer_norm_grad(x, dy, gain, stats, dx, dgain, dbias)
+    f32, t, dev, shape = torch.float32, x.dtype, x.device, x.shape
+    m, rows, cols = shape
+    dx = torch.empty(shape, dtype=t, device=dev) if dx is None else dx
+    dgain = torch.empty((m, cols), dtype=f32, device=dev) if dgain is None else dgain
+    dbias = torch.empty((m, cols), dtype=f32, device=dev) if dbias is None else dbias
+    _check(where, "stats", stats, (m, rows, 2), f32, dev)
+    if not stats.is_contiguous():
+        _refuse(where, "stats is not contiguous")
+    gp, gs = _vector(where, "gain", gain, (m, cols), f32, dev)
+    dgp, dgs = _vector(where, "dgain", dgain, (m, cols), f32, dev)
+    dbp, dbs = _vector(where, "dbias", dbias, (m, cols), f32, dev)
+    if m > 1 and dgs != dbs:
+        _refuse(where, "dgain and dbias have different distances between replicas")
+    L = lib()
+    n = L.lc_layer_norm_workspace_bytes(m, rows, cols)
+    ws = _workspace(n, dev)
+    rc = L.lc_layer_norm_grad(m, rows, cols, t is torch.bfloat16, _rows(where, "x", x, shape, t, dev), _rows(where, "dy", dy, shape, t, dev),
+                              gp, gs, stats.data_ptr(), _rows(where, "dx", dx, shape, t, dev), dgp, dbp, dgs, ws.data_ptr(), n,
+                              stream.cuda_stream)
+    if rc:
+        raise LcError(rc, where)
+    return dx, dgain, dbias
 
-    def go():
-        f32 = torch.float32
-        to = torch.empty_like(x, memory_format=torch.contiguous_format) if dx is None else dx
-        dg = torch.empty((m, cols), dtype=f32, device=x.device) if dgain is None else dgain
-        db = torch.empty((m, cols), dtype=f32, device=x.device) if dbias is None else dbias
-        c.check(stats, "stats", (m, rows, 2), f32)
-        _need(stats.is_contiguous(), c.where, "stats is not contiguous")
-        gp, gs = c.vector(gain, "gain", (m, cols), f32)
-        (dgp, dgs), (dbp, dbs) = c.vector(dg, "dgain", (m, cols), f32), c.vector(db, "dbias", (m, cols), f32)
-        _need(m == 1 or dgs == dbs, c.where, "dgain and dbias have different distances between replicas")
-        n = lib().lc_layer_norm_workspace_bytes(m, rows, cols)
-        ws = c.workspace(n)
-        c.status(lib().lc_layer_norm_grad(m, rows, cols, c.code(x.dtype), c.rows(x, "x", x.shape, x.dtype),
-                                          c.rows(dy, "dy", x.shape, x.dtype), gp, gs, stats.data_ptr(),
-                                          c.rows(to, "dx", x.shape, x.dtype), dgp, dbp, dgs, ws.data_ptr(), n,
-                                          c.stream.cuda_stream))
-        return to, dg, db
-    return c.run(go)
 
-
-def _softmax_head(where, A, W, bias, labels, grads, stream):
+def _softmax_head(where, A, W, bias, labels, stream, grads):
     import torch
-    c = _Call(where, A, _types(torch), stream)
-    _need(A.dim() == 3 and W.dim() == 3, where, "A is [m, rows, inputs], W [m, inputs, classes]")
+    f32, t, dev = torch.float32, A.dtype, A.device
     m, rows, d = A.shape
+    if W.dim() != 3:
+        _refuse(where, "W is [m, inputs, classes]")
     classes = W.shape[2]
-
-    def go():
-        f32 = torch.float32
-        h = LcHeadArgs(m=m, inputs=d, rows=rows, classes=classes, dtype=c.code(A.dtype))
-        h.A, h.W = c.rows(A, "A", A.shape, A.dtype), c.rows(W, "W", (m, d, classes), A.dtype)
-        h.bias, h.bias_replica = c.vector(bias, "bias", (m, classes), f32)
-        h.labels, h.label_replica = c.vector(labels, "labels", (m, rows), torch.int32)
-        loss = torch.empty(m, dtype=f32, device=A.device)
-        row_loss = torch.empty((m, rows), dtype=f32, device=A.device)
-        h.loss, h.row_loss, h.row_loss_replica = loss.data_ptr(), row_loss.data_ptr(), rows
-        if grads is None:
-            n = lib().lc_softmax_head_workspace_bytes(C.byref(h), 0)
-            ws = c.workspace(n)
-            c.status(lib().lc_softmax_head_loss(C.byref(h), ws.data_ptr(), n, c.stream.cuda_stream))
-            return loss, row_loss
+    h = LcHeadArgs(m=m, inputs=d, rows=rows, classes=classes, dtype=t is torch.bfloat16)
+    h.A, h.W = _rows(where, "A", A, A.shape, t, dev), _rows(where, "W", W, (m, d, classes), t, dev)
+    h.bias, h.bias_replica = _vector(where, "bias", bias, (m, classes), f32, dev)
+    h.labels, h.label_replica = _vector(where, "labels", labels, (m, rows), torch.int32, dev)
+    loss = torch.empty(m, dtype=f32, device=dev)
+    h.loss = loss.data_ptr()
+    L = lib()
+    if grads is None:
+        row_loss = torch.empty((m, rows), dtype=f32, device=dev)
+        h.row_loss, h.row_loss_replica = row_loss.data_ptr(), rows
+        out, fn = (loss, row_loss), L.lc_softmax_head_loss
+    else:
         dA, dW, db, dtype = grads
-        dtype = dtype or (dW.dtype if dW is not None else A.dtype)
-        _need(dtype in _types(torch), where, f"gradients of element type {dtype}")
-        dA = torch.empty((m, rows, d), dtype=A.dtype, device=A.device) if dA is None else dA
-        dW = torch.empty((m, d, classes), dtype=dtype, device=A.device) if dW is None else dW
-        db = torch.empty((m, classes), dtype=dtype, device=A.device) if db is None else db
-        h.grad_dtype = c.code(dtype)
-        h.dA, h.dW = c.rows(dA, "dA", A.shape, A.dtype), c.rows(dW, "dW", (m, d, classes), dtype)
-        h.db, h.db_replica = c.vector(db, "db", (m, classes), dtype)
-        n = lib().lc_softmax_head_workspace_bytes(C.byref(h), 1)
-        ws = c.workspace(n)
-        c.status(lib().lc_softmax_head_grad(C.byref(h), ws.data_ptr(), n, c.stream.cuda_stream))
-        return loss, dA, dW, db
-    return c.run(go)
+        dtype = dtype or (dW.dtype if dW is not None else t)
+        if dtype is not f32 and dtype is not torch.bfloat16:
+            _refuse(where, f"gradients of element type {dtype}")
+        dA = torch.empty((m, rows, d), dtype=t, device=dev) if dA is None else dA
+        dW = torch.empty((m, d, classes), dtype=dtype, device=dev) if dW is None else dW
+        db = torch.empty((m, classes), dtype=dtype, device=dev) if db is None else db
+        h.grad_dtype = dtype is torch.bfloat16
+        h.dA, h.dW = _rows(where, "dA", dA, A.shape, t, dev), _rows(where, "dW", dW, (m, d, classes), dtype, dev)
+        h.db, h.db_replica = _vector(where, "db", db, (m, classes), dtype, dev)
+        out, fn = (loss, dA, dW, db), L.lc_softmax_head_grad
+    n = L.lc_softmax_head_workspace_bytes(C.byref(h), grads is not None)
+    ws = _workspace(n, dev)
+    rc = fn(C.byref(h), ws.data_ptr(), n, stream.cuda_stream)
+    if rc:
+        raise LcError(rc, where)
+    return out
 
 
 def softmax_head_loss(A, W, bias, labels, stream=None):
     """lc_softmax_head_loss: mean cross-entropy [m] of Z = A W + bias and the rows' [m, rows]; A [m, rows, inputs] and
     W [m, inputs, classes] fp32 or bfloat16, bias fp32 [m, classes] or None, labels int32 [m, rows]."""
-    return _softmax_head("lc_softmax_head_loss", A, W, bias, labels, None, stream)
+    where = "lc_softmax_head_loss"
+    stream, other = _first(where, A, stream)
+    if other:
+        with _on(stream):
+            return _softmax_head(where, A, W, bias, labels, stream, None)
+    return _softmax_head(where, A, W, bias, labels, stream, None)
 
 
 def softmax_head_grad(A, W, bias, labels, dA=None, dW=None, db=None, grad_dtype=None, stream=None):
     """lc_softmax_head_grad: the loss [m], dA, dW and db (the last two of grad_dtype, A's element type by default)."""
-    return _softmax_head("lc_softmax_head_grad", A, W, bias, labels, (dA, dW, db, grad_dtype), stream)
+    where = "lc_softmax_head_grad"
+    stream, other = _first(where, A, stream)
+    if other:
+        with _on(stream):
+            return _softmax_head(where, A, W, bias, labels, stream, (dA, dW, db, grad_dtype))
+    return _softmax_head(where, A, W, bias, labels, stream, (dA, dW, db, grad_dtype))
 
 
 def orthogonalize(src, steps: int = 5, out=None, stream=None):
     """lc_orthogonalize of src [m, rows, cols], fp32 or bfloat16."""
     import torch
-    c = _Call("lc_orthogonalize", src, _types(torch), stream)
-    _need(src.dim() == 3, c.where, "src is [m, rows, cols]")
-    m, rows, cols = src.shape
-
-    def go():
-        to = torch.empty_like(src, memory_format=torch.contiguous_format) if out is None else out
-        n = lib().lc_orthogonal_workspace_bytes(m, rows, cols, c.code(src.dtype))
-        ws = c.workspace(n)
-        c.status(lib().lc_orthogonalize(m, rows, cols, c.code(src.dtype), c.rows(src, "src", src.shape, src.dtype),
-                                        c.rows(to, "out", src.shape, src.dtype), int(steps), ws.data_ptr(), n,
-                                        c.stream.cuda_stream))
-        return to
-    return c.run(go)
+    where = "lc_orthogonalize"
+    stream, other = _first(where, src, stream)
+    if other:
+        with _on(stream):
+            return orthogonalize(src, steps, out)
+    t, dev, shape = src.dtype, src.device, src.shape
+    m, rows, cols = shape
+    out = torch.empty(shape, dtype=t, device=dev) if out is None else out
+    L = lib()
+    n = L.lc_orthogonal_workspace_bytes(m, rows, cols, t is torch.bfloat16)
+    ws = _workspace(n, dev)
+    rc = L.lc_orthogonalize(m, rows, cols, t is torch.bfloat16, _rows(where, "src", src, shape, t, dev),
+                            _rows(where, "out", out, shape, t, dev), int(steps), ws.data_ptr(), n, stream.cuda_stream)
+    if rc:
+        raise LcError(rc, where)
+    return out
 
 
 def update_orthogonal(X, V, G, lr: float, beta: float, wd: float = 0.0, steps: int = 5, stream=None) -> None:
     """lc_update_orthogonal of X and V in place, fp32 [m, rows, cols] each."""
     import torch
-    c = _Call("lc_update_orthogonal", X, (torch.float32,), stream)
-    _need(X.dim() == 3, c.where, "X is [m, rows, cols]")
-    m, rows, cols = X.shape
-
-    def go():
-        n = lib().lc_orthogonal_workspace_bytes(m, rows, cols, GEMM_FP32)
-        ws = c.workspace(n)
-        c.status(lib().lc_update_orthogonal(m, rows, cols, *(c.rows(t, k, X.shape, X.dtype) for t, k in ((X, "X"), (V, "V"), (G, "G"))),
-                                            lr, beta, wd, int(steps), ws.data_ptr(), n, c.stream.cuda_stream))
-    c.run(go)
+    where = "lc_update_orthogonal"
+    stream, other = _first(where, X, stream)
+    if other:
+        with _on(stream):
+            return update_orthogonal(X, V, G, lr, beta, wd, steps)
+    f32, dev, shape = torch.float32, X.device, X.shape
+    m, rows, cols = shape
+    L = lib()
+    n = L.lc_orthogonal_workspace_bytes(m, rows, cols, GEMM_FP32)
+    ws = _workspace(n, dev)
+    rc = L.lc_update_orthogonal(m, rows, cols, *(_rows(where, k, t, shape, f32, dev) for t, k in ((X, "X"), (V, "V"), (G, "G"))),
+                                lr, beta, wd, int(steps), ws.data_ptr(), n, stream.cuda_stream)
+    if rc:
+        raise LcError(rc, where)
 
 
 class LocalSGD:

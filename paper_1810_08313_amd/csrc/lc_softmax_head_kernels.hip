@@ -310,22 +310,22 @@ struct DeltaArgs {
     const int32_t* label;
     const int* kept;
     int64_t label_rep;
-    int base, n, parts, classes, row_blocks;
+    int base, n, parts, classes, row_blocks, block_rows;
     float* db_part;              // [m][row_blocks][ep]
 };
 
-// 64 rows x 2048 classes a workgroup, 8 classes a thread, so that its columns' sums stay in registers.
+// block_rows rows x 2048 classes a workgroup, 8 classes a thread, so that its columns' sums stay in registers.
 template <typename E>
 __global__ void __launch_bounds__(kBlock) head_delta_kernel(DeltaArgs d) {
-    const int i = blockIdx.z, r0 = blockIdx.y * 64, c = (blockIdx.x * kBlock + threadIdx.x) * 8;
+    const int i = blockIdx.z, r0 = blockIdx.y * d.block_rows, c = (blockIdx.x * kBlock + threadIdx.x) * 8;
     const int kept = d.kept[i] - d.base;
     if (c >= d.ep) return;
     float sum[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[k] = 0.f;
-    if (r0 < kept) {
+    if (r0 < (kept + 63) / 64 * 64) {   // the last 64 that count are filled up with zeros
 #pragma unroll 2
-        for (int r = r0; r < r0 + 64; ++r) {
+        for (int r = r0; r < r0 + d.block_rows; ++r) {
             const int64_t at = ((int64_t)i * d.n + r) * d.ep + c;
             float v[8];
             if (r < kept) {
@@ -379,17 +379,6 @@ struct Across {
 };
 __device__ __forceinline__ float per_row(const int* kept, int i) { return 1.f / static_cast<float>(max(1, kept[i])); }
 
-template <typename G>
-__global__ void __launch_bounds__(kBlock) head_db_kernel(const float* part, int row_blocks, int64_t ep, int classes, Across x, G* db,
-                                                         int64_t db_rep) {
-    const int i = blockIdx.y, c = blockIdx.x * kBlock + threadIdx.x;
-    if (c >= classes) return;
-    float s = x.first ? 0.f : x.acc[i * ep + c];
-    for (int b = 0; b < row_blocks; ++b) s += part[((int64_t)i * row_blocks + b) * ep + c];
-    if (x.last) db[i * db_rep + c] = static_cast<G>(s * per_row(x.kept, i));
-    else x.acc[i * ep + c] = s;
-}
-
 // ------------------------------------------------------------------ dA
 
 // Shares of dZ W^T over the classes, [splits][m][n][d] in 32 bits.
@@ -418,23 +407,74 @@ __global__ void __launch_bounds__(S::kThreads) head_da_kernel(TileArgs a, float*
         }
 }
 
-// The shares added up, each row to its place; rows that do not count get zeros.
-template <typename T>
-__global__ void __launch_bounds__(kBlock) head_da_rows_kernel(const float* part, int splits, int m_all, int n, int d, const int32_t* order,
-                                                              int64_t order_rep, const int* kept, int base, T* dA, int64_t row, int64_t rep) {
-    const int i = blockIdx.y, r = blockIdx.x;
-    T* to = dA + i * rep + order[i * order_rep + base + r] * row;
-    const bool keep = base + r < kept[i];
-    const float unit = per_row(kept, i);
-    for (int c = threadIdx.x; c < d; c += kBlock) {
-        float s = 0.f;
-        if (keep)
-            for (int k = 0; k < splits; ++k) s += part[(((int64_t)k * m_all + i) * n + r) * d + c];
-        to[c] = static_cast<T>(s * unit);
+// What is left of a chunk: dA's shares added up, each row to its place (rows that do not count get zeros), and db.
+struct FinishArgs {
+    const float* da;             // [splits][replicas][n][d]
+    int splits, n, d, here;
+    const int32_t* order;
+    int64_t order_rep;
+    const int* kept;
+    int base;
+    void* dA;
+    int64_t da_row, da_rep;
+    const float* db_part;
+    int row_blocks, classes;
+    int64_t ep;
+    void* db;                    // or null
+    int64_t db_rep;
+};
+// Grid: (rows, then 256 classes a workgroup; replicas).
+template <typename T, typename G>
+__global__ void __launch_bounds__(kBlock) head_finish_kernel(FinishArgs f, Across x) {
+    const int i = blockIdx.y;
+    const float unit = per_row(f.kept, i);
+    if (static_cast<int>(blockIdx.x) < f.here) {
+        const int r = blockIdx.x;
+        T* to = static_cast<T*>(f.dA) + i * f.da_rep + f.order[i * f.order_rep + f.base + r] * f.da_row;
+        const bool keep = f.base + r < f.kept[i];
+        for (int c = threadIdx.x; c < f.d; c += kBlock) {
+            float s = 0.f;
+            if (keep) {
+#pragma unroll 8
+                for (int k = 0; k < f.splits; ++k) s += f.da[(((int64_t)k * gridDim.y + i) * f.n + r) * f.d + c];
+            }
+            to[c] = static_cast<T>(s * unit);
+        }
+        return;
     }
+    const int c = (blockIdx.x - f.here) * kBlock + threadIdx.x;
+    if (c >= f.classes) return;
+    float s = x.first ? 0.f : x.acc[i * f.ep + c];
+#pragma unroll 8
+    for (int b = 0; b < f.row_blocks; ++b) s += f.db_part[((int64_t)i * f.row_blocks + b) * f.ep + c];
+    if (x.last) static_cast<G*>(f.db)[i * f.db_rep + c] = static_cast<G>(s * unit);
+    else x.acc[i * f.ep + c] = s;
 }
 
 // ------------------------------------------------------------------ dW
+
+// Rows of a result that start anywhere: the tile goes through LDS, a wavefront stores a row at a time, in words of 32
+// bits from the first that is aligned (bf16 rows of an odd number of classes, 8 x 512 x 50257: element by element 425 us,
+// so DW_NEW).
+__device__ __forceinline__ void put(float* lds, const float (&v)[4]) { *reinterpret_cast<f32x4*>(lds) = f32x4{v[0], v[1], v[2], v[3]}; }
+__device__ __forceinline__ void put(bf16_t* lds, const float (&v)[4]) {
+    bf16x4 h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = static_cast<bf16_t>(v[e]);
+    *reinterpret_cast<bf16x4*>(lds) = h;
+}
+// `cols` (at most 256) elements from LDS to a row, a wavefront's work.
+__device__ __forceinline__ void store_row(const float* from, float* to, int cols, int lane) {
+    for (int c = lane; c < cols; c += 64) to[c] = from[c];
+}
+__device__ __forceinline__ void store_row(const bf16_t* from, bf16_t* to, int cols, int lane) {
+    const int odd = reinterpret_cast<uintptr_t>(to) >> 1 & 1;   // the first word's place
+    if (odd && lane == 0) to[0] = from[0];
+    for (int c = odd + 2 * lane; c < cols; c += 128) {
+        if (c + 1 < cols) *reinterpret_cast<uint32_t*>(to + c) = bits(from[c]) | static_cast<uint32_t>(bits(from[c + 1])) << 16;
+        else to[c] = from[c];
+    }
+}
 
 template <typename S, typename G>
 __global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across x, G* dW, int64_t row, int64_t rep, int vec) {
@@ -446,45 +486,66 @@ __global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across
     f32x4 acc[S::TM][S::TN];
     tile_sums<bf16_t, S, NMajor>(a, pl, k0, k1, lds, acc);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int mw = pl.tm * S::BM + (w / S::WN) * S::TM * 16 + (lane & 15), nw = pl.tn * S::BN + (w % S::WN) * S::TN * 16 + (lane >> 4) * 4;
+    const int mt = (w / S::WN) * S::TM * 16 + (lane & 15), nt = (w % S::WN) * S::TN * 16 + (lane >> 4) * 4;   // inside the tile
+    const int m0 = pl.tm * S::BM, n0 = pl.tn * S::BN;
     const float unit = per_row(x.kept, pl.batch);
+    // sums of the chunks so far
+    if (x.acc) {
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i)
+        for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j) {
-            const int m = mw + i * 16, n = nw + j * 16;
-            if (m >= a.M || n >= a.N) continue;
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e];
-            float* sum = x.acc ? x.acc + ((int64_t)pl.batch * a.M + m) * a.b.len + n : nullptr;   // rows of padded classes
-            if (!x.first) {
-                const f32x4 s = *reinterpret_cast<const f32x4*>(sum);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += s[e];
+            for (int j = 0; j < S::TN; ++j) {
+                const int m = m0 + mt + i * 16, n = n0 + nt + j * 16;
+                if (m >= a.M || n >= a.N) continue;
+                float* sum = x.acc + ((int64_t)pl.batch * a.M + m) * a.b.len + n;   // rows of padded classes
+                if (!x.first) acc[i][j] += *reinterpret_cast<const f32x4*>(sum);
+                if (!x.last) *reinterpret_cast<f32x4*>(sum) = acc[i][j];
             }
-            if (!x.last) {
-                *reinterpret_cast<f32x4*>(sum) = f32x4{v[0], v[1], v[2], v[3]};
-                continue;
+        if (!x.last) return;
+    }
+    dW += pl.batch * rep;
+    if (vec) {
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) {
+                const int m = m0 + mt + i * 16, n = n0 + nt + j * 16;
+                if (m >= a.M || n >= a.N) continue;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e] * unit;
+                G* to = dW + m * row + n;
+                if (n + 4 <= a.N) put(to, v);
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (n + e < a.N) to[e] = static_cast<G>(v[e]);
             }
+        return;
+    }
+    // a slice of 32 rows of every wavefront at a time, padded by 8 elements a row against bank conflicts
+    constexpr int kPitch = S::BN + 8, kSlice = 2, kRows = kSlice * 16 * S::WM;
+    static_assert(S::TM % kSlice == 0 && kRows * kPitch * sizeof(G) <= S::kLds * 2, "a slice fits the operands' buffers");
+    G* tile = reinterpret_cast<G*>(lds);
+    const int cols = min(S::BN, a.N - n0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] *= unit;
-            G* to = dW + pl.batch * rep + m * row + n;
-            if (vec && n + 4 <= a.N) {
-                if constexpr (sizeof(G) == 4) {
-                    *reinterpret_cast<f32x4*>(to) = f32x4{v[0], v[1], v[2], v[3]};
-                } else {
-                    bf16x4 h;
+    for (int i0 = 0; i0 < S::TM; i0 += kSlice) {
+        __syncthreads();
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) h[e] = static_cast<bf16_t>(v[e]);
-                    *reinterpret_cast<bf16x4*>(to) = h;
-                }
-            } else {
+        for (int i = 0; i < kSlice; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (n + e < a.N) to[e] = static_cast<G>(v[e]);
+            for (int j = 0; j < S::TN; ++j) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[i0 + i][j][e] * unit;
+                put(tile + ((w / S::WN) * kSlice * 16 + i * 16 + (lane & 15)) * kPitch + nt + j * 16, v);
             }
+        __syncthreads();
+        for (int r = w; r < kRows; r += S::kThreads / 64) {
+            const int m = m0 + r / (kSlice * 16) * S::TM * 16 + i0 * 16 + r % (kSlice * 16);
+            if (m < a.M) store_row(tile + r * kPitch, dW + m * row + n0, cols, lane);
         }
+    }
 }
 
 // ------------------------------------------------------------------ host
@@ -522,6 +583,7 @@ struct HeadPlan {
     int d, dp, cp, parts;        // inputs and padded, classes of a row of the copy of W, parts of a row's sum
     int64_t ep;                  // classes of a row of e
     int chunk, group, splits;    // rows and replicas at a time, shares of dA's product
+    int block_rows;
     int32_t *order, *label;
     int* kept;
     float *row_loss, *z_label, *coef, *delta_label, *da, *db_part, *db_acc, *dw_acc, *e32;
@@ -592,15 +654,18 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
         auto count = [&](auto) { tiles = (int64_t)t.mt * t.nt * g; };
         if (p.three) with_tile<true>(t, count);
         else with_tile<false>(t, count);
-        // few tiles: the classes are shared out until every compute unit has a share, of 8 tiles of k at least
-        p.splits = static_cast<int>(std::max<int64_t>(1, std::min((256 + tiles - 1) / tiles, p.ep / (8 * kPadK))));
+        // few tiles: the classes are shared out until every compute unit has a share, of 256 at least
+        p.splits = static_cast<int>(std::max<int64_t>(1, std::min((256 + tiles - 1) / tiles, p.ep / (4 * kPadK))));
         p.coef = c.take<float>(g * n * p.parts);
         p.delta_label = c.take<float>(g * n);
         p.at = c.take<uint16_t>(np * g * p.d * n);
         p.dz = c.take<uint16_t>(np * g * n * p.ep);
         p.e32 = c.take<float>(p.three ? g * n * p.ep : 0);
         p.da = c.take<float>(p.splits * g * n * p.d);
-        p.db_part = c.take<float>(g * (n / 64) * p.ep);
+        // rows of a workgroup that turns e into dZ: 64, fewer where that would leave compute units without one
+        p.block_rows = 64;
+        while (p.block_rows > 8 && g * (n / p.block_rows) * ((p.ep + kBlock * 8 - 1) / (kBlock * 8)) < 512) p.block_rows /= 2;
+        p.db_part = c.take<float>(g * (n / p.block_rows) * p.ep);
         p.db_acc = c.take<float>(chunks ? g * p.ep : 0);
         p.dw_acc = c.take<float>(chunks ? g * p.d * p.ep : 0);
     }
@@ -662,14 +727,11 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
                                                                             p.delta_label, row_loss + g0 * loss_rep, loss_rep);
             }
             if (!p.grad) continue;
-            const int row_blocks = (here + 63) / 64;
+            const int row_blocks = static_cast<int>(round_up(here, 64)) / p.block_rows;
             const DeltaArgs da{l.e, p.dz, p.ep, dz_part, p.coef, p.delta_label, label, kept, rows, base, static_cast<int>(n), p.parts,
-                               h.classes, row_blocks, p.db_part};
+                               h.classes, row_blocks, p.block_rows, p.db_part};
             if (here) head_delta_kernel<E><<<dim3(static_cast<unsigned>((p.ep + kBlock * 8 - 1) / (kBlock * 8)), row_blocks, g), kBlock, 0, st>>>(da);
             Across x{k == 0, k + 1 == chunks, p.db_acc, kept};
-            if (h.db)
-                head_db_kernel<G><<<dim3((h.classes + kBlock - 1) / kBlock, g), kBlock, 0, st>>>(
-                    p.db_part, row_blocks, p.ep, h.classes, x, static_cast<G*>(h.db) + g0 * h.db_replica, h.db_replica);
             // dA = dZ W^T
             t = TileArgs{};
             t.a = TileOperand{p.dz, p.ep, n * p.ep, {}, here, static_cast<int>(p.ep)};
@@ -687,9 +749,12 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
                     typedef decltype(s) S;
                     head_da_kernel<S><<<tile_grid(t), S::kThreads, 0, st>>>(t, p.da, static_cast<int>(n), p.d);
                 });
-                head_da_rows_kernel<T><<<dim3(here, g), kBlock, 0, st>>>(p.da, p.splits, g, static_cast<int>(n), p.d, order, rows, kept, base,
-                                                                         static_cast<T*>(h.dA.p) + g0 * h.dA.replica, h.dA.row, h.dA.replica);
             }
+            const FinishArgs fa{p.da, p.splits, static_cast<int>(n), p.d, here, order, rows, kept, base, static_cast<T*>(h.dA.p) + g0 * h.dA.replica,
+                                h.dA.row, h.dA.replica, p.db_part, row_blocks, h.classes, p.ep,
+                                h.db ? static_cast<G*>(h.db) + g0 * h.db_replica : nullptr, h.db_replica};
+            const unsigned finish = here + (h.db ? (h.classes + kBlock - 1) / kBlock : 0);
+            if (finish) head_finish_kernel<T, G><<<dim3(finish, g), kBlock, 0, st>>>(fa, x);
             // dW = A^T dZ
             t = TileArgs{};
             t.a = TileOperand{p.at, n, p.d * n, {}, p.d, static_cast<int>(n)};
