@@ -171,16 +171,16 @@ struct LogitArgs {
     int64_t ep;
 };
 
-template <typename S, typename E>
+template <typename S, typename E, BLayout LB>
 __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, LogitArgs l) {
     static_assert(S::BN == kWide, "a row's part is a workgroup's");
     __shared__ __align__(1024) uint16_t lds[S::kLds];
-    const TilePlace pl = tile_place(a);
+    const TilePlace pl = tile_place<S>(a);
     if (pl.batch < 0) return;
     const int kept = __builtin_amdgcn_readfirstlane(l.kept[pl.batch]) - l.base;
     if (pl.tm * S::BM >= kept) return;
     f32x4 acc[S::TM][S::TN];
-    tile_sums<bf16_t, S, NMajor>(a, pl, 0, a.K / S::BK, lds, acc);
+    tile_sums<bf16_t, S, LB>(a, pl, 0, a.K / S::BK, lds, acc);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w / S::WN, wn = w % S::WN;
     const int nw = pl.tn * S::BN + wn * S::TN * 16 + (lane >> 4) * 4;
     const float* bias = l.bias ? l.bias + pl.batch * l.bias_rep : nullptr;
@@ -381,17 +381,17 @@ __device__ __forceinline__ float per_row(const int* kept, int i) { return 1.f / 
 
 // ------------------------------------------------------------------ dA
 
-// Shares of dZ W^T over the classes, [splits][m][n][d] in 32 bits.
-template <typename S>
+// Shares of dZ W^T over the classes, [splits][m][n][d] in 32 bits, d padded to 4.
+template <typename S, BLayout LB>
 __global__ void __launch_bounds__(S::kThreads) head_da_kernel(TileArgs a, float* out, int n_rows, int d) {
     __shared__ __align__(1024) uint16_t lds[S::kLds];
-    const TilePlace pl = tile_place(a);
+    const TilePlace pl = tile_place<S>(a);
     if (pl.batch < 0) return;
     int k0, k1;
     tile_k_range<S>(a, pl, k0, k1);
     if (a.m_count && pl.tm * S::BM >= __builtin_amdgcn_readfirstlane(a.m_count[pl.batch]) - a.count_base) return;
     f32x4 acc[S::TM][S::TN];
-    tile_sums<bf16_t, S, KMajor>(a, pl, k0, k1, lds, acc);
+    tile_sums<bf16_t, S, LB>(a, pl, k0, k1, lds, acc);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int mw = pl.tm * S::BM + (w / S::WN) * S::TM * 16 + (lane & 15), nw = pl.tn * S::BN + (w % S::WN) * S::TN * 16 + (lane >> 4) * 4;
     out += ((int64_t)pl.split * a.batches + pl.batch) * n_rows * d;
@@ -400,17 +400,14 @@ __global__ void __launch_bounds__(S::kThreads) head_da_kernel(TileArgs a, float*
 #pragma unroll
         for (int j = 0; j < S::TN; ++j) {
             const int m = mw + i * 16, n = nw + j * 16;
-            if (m >= a.M) continue;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e < d) out[(int64_t)m * d + n + e] = acc[i][j][e];
+            if (m < a.M && n < d) *reinterpret_cast<f32x4*>(out + (int64_t)m * d + n) = acc[i][j];
         }
 }
 
 // What is left of a chunk: dA's shares added up, each row to its place (rows that do not count get zeros), and db.
 struct FinishArgs {
-    const float* da;             // [splits][replicas][n][d]
-    int splits, n, d, here;
+    const float* da;             // [splits][replicas][n][d4]
+    int splits, n, d, d4, here;
     const int32_t* order;
     int64_t order_rep;
     const int* kept;
@@ -436,7 +433,7 @@ __global__ void __launch_bounds__(kBlock) head_finish_kernel(FinishArgs f, Acros
             float s = 0.f;
             if (keep) {
 #pragma unroll 8
-                for (int k = 0; k < f.splits; ++k) s += f.da[(((int64_t)k * gridDim.y + i) * f.n + r) * f.d + c];
+                for (int k = 0; k < f.splits; ++k) s += f.da[(((int64_t)k * gridDim.y + i) * f.n + r) * f.d4 + c];
             }
             to[c] = static_cast<T>(s * unit);
         }
@@ -453,99 +450,55 @@ __global__ void __launch_bounds__(kBlock) head_finish_kernel(FinishArgs f, Acros
 
 // ------------------------------------------------------------------ dW
 
-// Rows of a result that start anywhere: the tile goes through LDS, a wavefront stores a row at a time, in words of 32
-// bits from the first that is aligned (bf16 rows of an odd number of classes, 8 x 512 x 50257: element by element 425 us,
-// so DW_NEW).
-__device__ __forceinline__ void put(float* lds, const float (&v)[4]) { *reinterpret_cast<f32x4*>(lds) = f32x4{v[0], v[1], v[2], v[3]}; }
-__device__ __forceinline__ void put(bf16_t* lds, const float (&v)[4]) {
-    bf16x4 h;
+// 8 values to consecutive places, wherever those start: one or two stores of 16 bytes.
+__device__ __forceinline__ void store8(float* to, const float (&v)[8]) { __builtin_memcpy(to, v, 32); }
+__device__ __forceinline__ void store8(bf16_t* to, const float (&v)[8]) {
+    bf16x8 h;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) h[e] = static_cast<bf16_t>(v[e]);
-    *reinterpret_cast<bf16x4*>(lds) = h;
-}
-// `cols` (at most 256) elements from LDS to a row, a wavefront's work.
-__device__ __forceinline__ void store_row(const float* from, float* to, int cols, int lane) {
-    for (int c = lane; c < cols; c += 64) to[c] = from[c];
-}
-__device__ __forceinline__ void store_row(const bf16_t* from, bf16_t* to, int cols, int lane) {
-    const int odd = reinterpret_cast<uintptr_t>(to) >> 1 & 1;   // the first word's place
-    if (odd && lane == 0) to[0] = from[0];
-    for (int c = odd + 2 * lane; c < cols; c += 128) {
-        if (c + 1 < cols) *reinterpret_cast<uint32_t*>(to + c) = bits(from[c]) | static_cast<uint32_t>(bits(from[c + 1])) << 16;
-        else to[c] = from[c];
-    }
+    for (int e = 0; e < 8; ++e) h[e] = static_cast<bf16_t>(v[e]);
+    __builtin_memcpy(to, &h, 16);
 }
 
 template <typename S, typename G>
-__global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across x, G* dW, int64_t row, int64_t rep, int vec) {
+__global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across x, G* dW, int64_t row, int64_t rep) {
     __shared__ __align__(1024) uint16_t lds[S::kLds];
-    const TilePlace pl = tile_place(a);
+    const TilePlace pl = tile_place<S>(a);
     if (pl.batch < 0) return;
     int k0, k1;
     tile_k_range<S>(a, pl, k0, k1);
     f32x4 acc[S::TM][S::TN];
     tile_sums<bf16_t, S, NMajor>(a, pl, k0, k1, lds, acc);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int mt = (w / S::WN) * S::TM * 16 + (lane & 15), nt = (w % S::WN) * S::TN * 16 + (lane >> 4) * 4;   // inside the tile
-    const int m0 = pl.tm * S::BM, n0 = pl.tn * S::BN;
+    const int m0 = pl.tm * S::BM, n0 = pl.tn * S::BN, cols = min(S::BN, a.N - n0);
     const float unit = per_row(x.kept, pl.batch);
-    // sums of the chunks so far
-    if (x.acc) {
-#pragma unroll
-        for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-            for (int j = 0; j < S::TN; ++j) {
-                const int m = m0 + mt + i * 16, n = n0 + nt + j * 16;
-                if (m >= a.M || n >= a.N) continue;
-                float* sum = x.acc + ((int64_t)pl.batch * a.M + m) * a.b.len + n;   // rows of padded classes
-                if (!x.first) acc[i][j] += *reinterpret_cast<const f32x4*>(sum);
-                if (!x.last) *reinterpret_cast<f32x4*>(sum) = acc[i][j];
-            }
-        if (!x.last) return;
-    }
     dW += pl.batch * rep;
-    if (vec) {
+    const SumSlices<S> sums(lds);
+    each_slice<S>([&](auto slice) {
+        constexpr int SL = decltype(slice)::value;
+        sums.template put<SL>(acc);
+        sums.rows8([](int, int, int) {}, [&](int, int r, int c, float (&v)[8]) {
+            const int m = m0 + sums.row_of(SL, r);
+            if (m >= a.M || c >= cols) return false;
+            f32x4* sum = reinterpret_cast<f32x4*>(x.acc + ((int64_t)pl.batch * a.M + m) * a.b.len + n0 + c);   // rows of padded classes
+            if (!x.first) {
 #pragma unroll
-        for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-            for (int j = 0; j < S::TN; ++j) {
-                const int m = m0 + mt + i * 16, n = n0 + nt + j * 16;
-                if (m >= a.M || n >= a.N) continue;
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e] * unit;
-                G* to = dW + m * row + n;
-                if (n + 4 <= a.N) put(to, v);
-                else
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (n + e < a.N) to[e] = static_cast<G>(v[e]);
+                for (int e = 0; e < 4; ++e) v[e] += sum[0][e], v[4 + e] += sum[1][e];
             }
-        return;
-    }
-    // a slice of 32 rows of every wavefront at a time, padded by 8 elements a row against bank conflicts
-    constexpr int kPitch = S::BN + 8, kSlice = 2, kRows = kSlice * 16 * S::WM;
-    static_assert(S::TM % kSlice == 0 && kRows * kPitch * sizeof(G) <= S::kLds * 2, "a slice fits the operands' buffers");
-    G* tile = reinterpret_cast<G*>(lds);
-    const int cols = min(S::BN, a.N - n0);
-#pragma unroll
-    for (int i0 = 0; i0 < S::TM; i0 += kSlice) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kSlice; ++i)
-#pragma unroll
-            for (int j = 0; j < S::TN; ++j) {
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[i0 + i][j][e] * unit;
-                put(tile + ((w / S::WN) * kSlice * 16 + i * 16 + (lane & 15)) * kPitch + nt + j * 16, v);
+            if (!x.last) {
+                sum[0] = f32x4{v[0], v[1], v[2], v[3]};
+                sum[1] = f32x4{v[4], v[5], v[6], v[7]};
+                return false;
             }
-        __syncthreads();
-        for (int r = w; r < kRows; r += S::kThreads / 64) {
-            const int m = m0 + r / (kSlice * 16) * S::TM * 16 + i0 * 16 + r % (kSlice * 16);
-            if (m < a.M) store_row(tile + r * kPitch, dW + m * row + n0, cols, lane);
-        }
-    }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= unit;
+            G* to = dW + m * row + n0 + c;
+            if (c + 8 <= cols) store8(to, v);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < cols) to[e] = static_cast<G>(v[e]);
+            return false;
+        });
+    });
 }
 
 // ------------------------------------------------------------------ host
@@ -569,8 +522,7 @@ template <bool THREE, typename F>
 void with_tile(TileArgs& a, F f) {
     auto go = [&](auto shape) {
         typedef decltype(shape) S;
-        a.mt = (a.M + S::BM - 1) / S::BM;
-        a.nt = (a.N + S::BN - 1) / S::BN;
+        tile_grid<S>(a);
         f(shape);
     };
     if (a.M <= 64) go(typename Tiles<THREE>::Rows64());
@@ -579,8 +531,8 @@ void with_tile(TileArgs& a, F f) {
 }
 
 struct HeadPlan {
-    bool grad, three, copy_w;    // gradients; fp32 operands in three parts; W copied first
-    int d, dp, cp, parts;        // inputs and padded, classes of a row of the copy of W, parts of a row's sum
+    bool grad, three, copy_w, any_w;   // gradients; fp32 operands in three parts; W copied first, or of any alignment
+    int d, dp, d4, cp, parts;    // inputs and padded, classes of a row of the copy of W, parts of a row's sum
     int64_t ep;                  // classes of a row of e
     int chunk, group, splits;    // rows and replicas at a time, shares of dA's product
     int block_rows;
@@ -622,11 +574,14 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
     p.three = h.dtype == LC_GEMM_FP32;
     p.d = h.inputs;
     p.dp = static_cast<int>(round_up(h.inputs, kPadK));
+    p.d4 = static_cast<int>(round_up(h.inputs, 4));
     p.parts = static_cast<int>((h.classes + kWide - 1) / kWide);
     p.ep = round_up(h.classes, kPadK);
-    // bf16 weights are read where they stand if every row starts on 16 bytes and holds whole chunks of 8
-    p.copy_w = p.three || h.classes % 8 || !aligned_to(h.W.p, 16) || (h.inputs > 1 && h.W.row % 8) || (h.m > 1 && h.W.replica % 8) ||
-               h.W.row > kMaxRowStride;
+    // bf16 weights are read where they stand: straight into LDS if every row starts on 16 bytes and holds whole chunks of 8,
+    // through registers otherwise (8 x 128 rows, 512 x 50257: a copy first cost 207 us of 860)
+    p.any_w = !p.three && (h.classes % 8 || !aligned_to(h.W.p, 16) || (h.inputs > 1 && h.W.row % 8) || (h.m > 1 && h.W.replica % 8));
+    p.copy_w = p.three || h.classes < 8 || (h.inputs > 1 && h.W.row > kMaxRowStride);
+    if (p.copy_w) p.any_w = false;
     p.cp = static_cast<int>(round_up(h.classes, 8));
     // rows and replicas at a time: bytes of a row's e (fp32: and of its dZ in parts), or of its parts' sums
     const int64_t per_row = grad ? p.ep * (p.three ? 10 : 2) : p.parts * 8;
@@ -651,7 +606,7 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
         t.M = static_cast<int>(n);
         t.N = p.d;
         int64_t tiles = 1;
-        auto count = [&](auto) { tiles = (int64_t)t.mt * t.nt * g; };
+        auto count = [&](auto) { tiles = (int64_t)t.per_batch * g; };
         if (p.three) with_tile<true>(t, count);
         else with_tile<false>(t, count);
         // few tiles: the classes are shared out until every compute unit has a share, of 256 at least
@@ -661,7 +616,7 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
         p.at = c.take<uint16_t>(np * g * p.d * n);
         p.dz = c.take<uint16_t>(np * g * n * p.ep);
         p.e32 = c.take<float>(p.three ? g * n * p.ep : 0);
-        p.da = c.take<float>(p.splits * g * n * p.d);
+        p.da = c.take<float>(p.splits * g * n * p.d4);
         // rows of a workgroup that turns e into dZ: 64, fewer where that would leave compute units without one
         p.block_rows = 64;
         while (p.block_rows > 8 && g * (n / p.block_rows) * ((p.ep + kBlock * 8 - 1) / (kBlock * 8)) < 512) p.block_rows /= 2;
@@ -721,7 +676,13 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             if (here) {
                 with_tile<sizeof(T) == 4>(t, [&](auto s) {
                     typedef decltype(s) S;
-                    head_logits_kernel<S, E><<<tile_grid(t), S::kThreads, 0, st>>>(t, l);
+                    if constexpr (sizeof(T) == 2) {
+                        if (p.any_w) {
+                            head_logits_kernel<S, E, NMajorAny><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, l);
+                            return;
+                        }
+                    }
+                    head_logits_kernel<S, E, NMajor><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, l);
                 });
                 head_join_kernel<<<dim3((here + 3) / 4, g), kBlock, 0, st>>>(l, order, p.three ? 1.f : 1.f / kEScale, p.coef,
                                                                             p.delta_label, row_loss + g0 * loss_rep, loss_rep);
@@ -747,10 +708,16 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             if (here) {
                 with_tile<sizeof(T) == 4>(t, [&](auto s) {
                     typedef decltype(s) S;
-                    head_da_kernel<S><<<tile_grid(t), S::kThreads, 0, st>>>(t, p.da, static_cast<int>(n), p.d);
+                    if constexpr (sizeof(T) == 2) {
+                        if (p.any_w) {
+                            head_da_kernel<S, KMajorAny><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, p.da, static_cast<int>(n), p.d4);
+                            return;
+                        }
+                    }
+                    head_da_kernel<S, KMajor><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, p.da, static_cast<int>(n), p.d4);
                 });
             }
-            const FinishArgs fa{p.da, p.splits, static_cast<int>(n), p.d, here, order, rows, kept, base, static_cast<T*>(h.dA.p) + g0 * h.dA.replica,
+            const FinishArgs fa{p.da, p.splits, static_cast<int>(n), p.d, p.d4, here, order, rows, kept, base, static_cast<T*>(h.dA.p) + g0 * h.dA.replica,
                                 h.dA.row, h.dA.replica, p.db_part, row_blocks, h.classes, p.ep,
                                 h.db ? static_cast<G*>(h.db) + g0 * h.db_replica : nullptr, h.db_replica};
             const unsigned finish = here + (h.db ? (h.classes + kBlock - 1) / kBlock : 0);
@@ -769,11 +736,9 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             t.count_base = base;
             x.acc = p.dw_acc;
             G* dW = static_cast<G*>(h.dW.p) + g0 * h.dW.replica;
-            const size_t gb = 4 * sizeof(G);
-            const int vec = aligned_to(dW, gb) && h.dW.row % 4 == 0 && (h.m == 1 || h.dW.replica % 4 == 0);
             with_tile<sizeof(T) == 4>(t, [&](auto s) {
                 typedef decltype(s) S;
-                head_dw_kernel<S, G><<<tile_grid(t), S::kThreads, 0, st>>>(t, x, dW, h.dW.row, h.dW.replica, vec);
+                head_dw_kernel<S, G><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, x, dW, h.dW.row, h.dW.replica);
             });
         }
     }

@@ -18,6 +18,8 @@
 // 8 x 4 tiles of an XCD share them: 0.9 ms alone), LDS reads and the matrix cores could do 0.5 and 0.7 ms: 1.16 ms
 // together, 945 TFLOP/s.  Tiles of 32 k in four buffers: 844.
 #pragma once
+#include <type_traits>
+
 #include "lc_internal.h"
 
 namespace lc {
@@ -54,14 +56,19 @@ constexpr int64_t kMaxRowStride = 1 << 22;   // offsets inside a tile of 256 row
 struct TileArgs {
     TileOperand a, b;
     int M, N, K;                  // K: padded to 64, A is zero behind its own length
-    int batches, mt, nt, splits;  // tiles in M and N, shares of the K axis
-    int upper;                    // symmetric result: only tiles with tm <= tn, (mt (mt + 1) / 2 of them)
+    int batches, splits;          // shares of the K axis
+    int mt, nt, per_batch;        // tiles in M, in N and of a batch; tile_grid() sets them
+    int upper;                    // symmetric result: only tiles that reach the diagonal or lie above it
     const int* m_count;           // [batches] rows of A that count, or null; tiles behind them run no product
     const int* k_count;           // [batches] k that count (a multiple of 64 is taken), or null
     int count_base;               // first row of the chunk: what is left of a count is max(0, count - base)
 };
 
-enum BLayout { KMajor, NMajor };
+// ...Any: rows that start anywhere and hold any number of elements; they come through registers, since what goes
+// straight into LDS has to be aligned.
+enum BLayout { KMajor, NMajor, KMajorAny, NMajorAny };
+constexpr bool n_contiguous(BLayout l) { return l == NMajor || l == NMajorAny; }
+constexpr bool any_alignment(BLayout l) { return l == KMajorAny || l == NMajorAny; }
 
 template <int BM_, int BN_, int WM_, int WN_, int BK_, int NP_, int STAGES_>
 struct TileShape {
@@ -74,7 +81,7 @@ struct TileShape {
     static constexpr int kStages = STAGES_, kLds = kStages * kStage;
     static constexpr int kLoads = kStage / 8 / kThreads;           // load instructions of a thread for a buffer
     static_assert(kPart % (8 * kThreads) == 0 && kLoads * (kStages - 2) < 64, "what a wait can count");
-    static_assert(BM * BK % (8 * kThreads) == 0 && kLds * 2 <= 160 * 1024 && TM % 2 == 0 && TN % 2 == 0, "");
+    static_assert(BM * BK % (8 * kThreads) == 0 && kLds * 2 <= 160 * 1024 && TM % 2 == 0, "");
 };
 
 typedef __attribute__((address_space(3))) void* LdsPtr;
@@ -170,6 +177,51 @@ __device__ __forceinline__ s16x8 read_nmajor(const uint16_t* tile, int col, int 
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
+// The same through registers: load() asks, commit() writes to LDS what has come.  `len` is any length of at least 8.
+template <int R, int BK, int THREADS, bool NMAJOR>
+struct AnyFetch {
+    static constexpr int kAcross = NMAJOR ? R : BK, kChunks = kAcross / 8, kPer = THREADS / kChunks, kLoads = (NMAJOR ? BK : R) / kPer;
+    u32x4 reg[kLoads];
+    int r0, x0, c;   // the lane's row (and chunk) inside the tile; the chunk's first place
+    __device__ __forceinline__ void init(const TileOperand&, int first) {
+        const int t = threadIdx.x;
+        r0 = t / kChunks;
+        x0 = first;
+        c = t % kChunks;
+    }
+    // `base`: the operand's first element (NMAJOR), or the tile's first row
+    __device__ __forceinline__ void load(const TileOperand& o, const char* base, int k0) {
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) {
+            const int r = q * kPer + r0;
+            int row, x;
+            if constexpr (NMAJOR) {
+                row = min(k0 + r, o.rows - 1);
+                x = x0 + (c ^ NMajorFetch<R, BK, THREADS>::swizzle(r)) * 8;
+            } else {
+                row = min(x0 + r, o.rows - 1) - x0;
+                x = k0 + (BK == 64 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3)) * 8;
+            }
+            const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + (int64_t)row * o.row;
+            if (x + 8 <= o.len) {
+                __builtin_memcpy(&reg[q], p + x, 16);
+            } else {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t lo = x + 2 * e < o.len ? p[x + 2 * e] : 0, hi = x + 2 * e + 1 < o.len ? p[x + 2 * e + 1] : 0;
+                    w[e] = lo | hi << 16;
+                }
+                reg[q] = u32x4{w[0], w[1], w[2], w[3]};
+            }
+        }
+    }
+    __device__ __forceinline__ void commit(uint16_t* to) const {
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) *reinterpret_cast<u32x4*>(to + (q * THREADS + threadIdx.x) * 8) = reg[q];
+    }
+};
+
 template <BLayout L, typename S>
 struct FetchB {
     typedef KMajorFetch<S::BN, S::BK, S::kThreads> type;
@@ -178,31 +230,52 @@ template <typename S>
 struct FetchB<NMajor, S> {
     typedef NMajorFetch<S::BN, S::BK, S::kThreads> type;
 };
+template <typename S>
+struct FetchB<KMajorAny, S> {
+    typedef AnyFetch<S::BN, S::BK, S::kThreads, false> type;
+};
+template <typename S>
+struct FetchB<NMajorAny, S> {
+    typedef AnyFetch<S::BN, S::BK, S::kThreads, true> type;
+};
 
 struct TilePlace {
     int batch, tm, tn, split;   // batch < 0: nothing to do
 };
 
+// Tiles of a symmetric result in column tn: those whose first row is not behind the column's last n.
+__host__ __device__ __forceinline__ int upper_tiles(int tn, int bm, int bn, int mt) {
+    const int c = ((tn + 1) * bn + bm - 1) / bm;
+    return c < mt ? c : mt;
+}
+__host__ __device__ __forceinline__ int64_t tiles_of(const TileArgs& a, int bm, int bn) {
+    if (!a.upper) return (int64_t)a.mt * a.nt;
+    int64_t n = 0;
+    for (int tn = 0; tn < a.nt; ++tn) n += upper_tiles(tn, bm, bn, a.mt);
+    return n;
+}
+// Whether element (m, n) above the diagonal has to be stored at (n, m) as well: no tile covers that.
+template <typename S>
+__device__ __forceinline__ bool mirrored(int m, int n) { return n / S::BM * S::BM >= (m / S::BN + 1) * S::BN; }
+
 // Workgroup id -> tile.  Each XCD takes a contiguous range; inside it, blocks of 8 tiles of M by all of N, M fastest,
 // so that what runs together shares rows of A and columns of B in the L2.
+template <typename S>
 __device__ __forceinline__ TilePlace tile_place(const TileArgs& a) {
-    const int per = a.upper ? a.mt * (a.mt + 1) / 2 : a.mt * a.nt;
-    const int64_t total = (int64_t)per * a.batches * a.splits;
+    const int64_t total = (int64_t)a.per_batch * a.batches * a.splits;
     const int64_t chunk = (total + kXcds - 1) / kXcds;
     const int64_t id = (int64_t)(blockIdx.x % kXcds) * chunk + blockIdx.x / kXcds;
     TilePlace pl{-1, 0, 0, 0};
     if (blockIdx.x / kXcds >= chunk || id >= total) return pl;
-    const int64_t one = id % ((int64_t)per * a.splits);
-    pl.batch = (int)(id / ((int64_t)per * a.splits));
-    pl.split = (int)(one / per);
-    const int t = (int)(one % per);
+    const int64_t one = id % ((int64_t)a.per_batch * a.splits);
+    pl.batch = (int)(id / ((int64_t)a.per_batch * a.splits));
+    pl.split = (int)(one / a.per_batch);
+    int t = (int)(one % a.per_batch);
     if (a.upper) {
-        // column tn holds tn + 1 tiles
-        int tn = __builtin_amdgcn_readfirstlane((int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f));
-        while ((tn + 1) * (tn + 2) / 2 <= t) ++tn;
-        while (tn * (tn + 1) / 2 > t) --tn;
+        int tn = 0;
+        for (int c; (c = upper_tiles(tn, S::BM, S::BN, a.mt)) <= t; ++tn) t -= c;
         pl.tn = tn;
-        pl.tm = t - tn * (tn + 1) / 2;
+        pl.tm = t;
     } else {
         constexpr int kG = 8;
         const int g = t / (kG * a.nt), first = g * kG, size = min(kG, a.mt - first);
@@ -212,9 +285,13 @@ __device__ __forceinline__ TilePlace tile_place(const TileArgs& a) {
     return pl;
 }
 
-inline unsigned tile_grid(const TileArgs& a) {
-    const int64_t per = a.upper ? (int64_t)a.mt * (a.mt + 1) / 2 : (int64_t)a.mt * a.nt;
-    const int64_t total = per * a.batches * a.splits;
+// Numbers of tiles for shape S, and the grid.
+template <typename S>
+inline unsigned tile_grid(TileArgs& a) {
+    a.mt = (a.M + S::BM - 1) / S::BM;
+    a.nt = (a.N + S::BN - 1) / S::BN;
+    a.per_batch = (int)tiles_of(a, S::BM, S::BN);
+    const int64_t total = (int64_t)a.per_batch * a.batches * a.splits;
     return (unsigned)((total + kXcds - 1) / kXcds * kXcds);
 }
 
@@ -245,33 +322,47 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (total <= 0) return;
     const char* ab = reinterpret_cast<const char*>(a.a.p + (int64_t)pl.batch * a.a.batch + (int64_t)m0 * a.a.row);
-    const char* bb = reinterpret_cast<const char*>(a.b.p + (int64_t)pl.batch * a.b.batch + (L == KMajor ? (int64_t)n0 * a.b.row : 0));
+    const char* bb = reinterpret_cast<const char*>(a.b.p + (int64_t)pl.batch * a.b.batch + (n_contiguous(L) ? 0 : (int64_t)n0 * a.b.row));
     KMajorFetch<S::BM, S::BK, S::kThreads> fetch_a;
     typename FetchB<L, S>::type fetch_b;
     fetch_a.init(a.a, m0);
     fetch_b.init(a.b, n0);
     constexpr int NS = S::kStages, NP = S::NP, KS = S::KS;
+    constexpr bool ANY = any_alignment(L);
+    static_assert(!ANY || NP == 1, "");
+    constexpr int kCounted = ANY ? S::BM * S::BK / 8 / S::kThreads : S::kLoads;   // loads of a tile that go straight into LDS
     int next_k = kt0 * S::BK, next_buf = 0;   // of the tile that is fetched next
     auto ask_a = [&] {
 #pragma unroll
         for (int p = 0; p < NP; ++p) fetch_a.fetch(a.a, ab + 2 * a.a.part[p], next_k, lds + next_buf * S::kStage + p * S::kPart);
     };
+    uint16_t* pending = nullptr;
     auto ask_b = [&] {
+        if constexpr (ANY) {
+            fetch_b.load(a.b, bb, next_k);
+            pending = lds + next_buf * S::kStage + S::BM * S::BK;
+        } else {
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
-            fetch_b.fetch(a.b, bb + 2 * a.b.part[p], next_k, lds + next_buf * S::kStage + p * S::kPart + S::BM * S::BK);
+            for (int p = 0; p < NP; ++p)
+                fetch_b.fetch(a.b, bb + 2 * a.b.part[p], next_k, lds + next_buf * S::kStage + p * S::kPart + S::BM * S::BK);
+        }
         next_k += S::BK;
         next_buf = next_buf + 1 == NS ? 0 : next_buf + 1;
+    };
+    auto commit_b = [&] {
+        if constexpr (ANY) fetch_b.commit(pending);
     };
     const int ahead = min(NS - 1, total);
     for (int t = 0; t < ahead; ++t) {
         ask_a();
         ask_b();
+        commit_b();
     }
+    if constexpr (ANY) __builtin_amdgcn_s_waitcnt(kWaitLds);
     int buf = 0;
     // a quarter of the wavefront's tile at a time: half of its rows by half of its columns, all parts and 32-deep steps
-    constexpr int HM = S::TM / 2, HN = S::TN / 2;
-    s16x8 fa[HM][NP][KS], fb[2][HN][NP][KS];
+    constexpr int HM = S::TM / 2, NH = S::TN % 2 ? 1 : 2, HN = S::TN / NH;   // (an odd number of columns: half)
+    s16x8 fa[HM][NP][KS], fb[NH][HN][NP][KS];
     auto read_b = [&](const uint16_t* tb, int h) {
 #pragma unroll
         for (int p = 0; p < NP; ++p)
@@ -279,7 +370,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
                 for (int j = 0; j < HN; ++j) {
-                    if constexpr (L == KMajor)
+                    if constexpr (!n_contiguous(L))
                         fb[h][j][p][ks] = read_kmajor<S::BK>(tb + p * S::kPart, (wn * S::TN + h * HN + j) * 16, ks, lane);
                     else
                         fb[h][j][p][ks] = read_nmajor<S::BN>(tb + p * S::kPart, (wn * S::TN + h * HN + j) * 16, ks, lane);
@@ -315,7 +406,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         tile_barrier();
     };
     auto oldest = [&](int asked) {   // tiles asked for beyond the one that is waited for
-        if (asked == NS - 2) __builtin_amdgcn_s_waitcnt(wait_loads((NS - 2) * S::kLoads));
+        if (asked == NS - 2) __builtin_amdgcn_s_waitcnt(wait_loads((NS - 2) * kCounted));
         else __builtin_amdgcn_s_waitcnt(wait_loads(0));
     };
     if constexpr (S::WM * S::WN == 8) {
@@ -330,14 +421,24 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
             read_b(tb, 0);
             read_a(ta, 0);
             if (more) ask_a();
-            turn(0, 0);
-            read_b(tb, 1);
-            if (more) ask_b();
-            turn(0, 1);
-            read_a(ta, 1);
-            turn(1, 1);
-            oldest(more ? NS - 2 : 0);
-            turn(1, 0);
+            if constexpr (NH == 2) {
+                turn(0, 0);
+                read_b(tb, 1);
+                if (more) ask_b();
+                turn(0, 1);
+                read_a(ta, 1);
+                turn(1, 1);
+                if (more) commit_b();
+                oldest(more ? NS - 2 : 0);
+                turn(1, 0);
+            } else {
+                if (more) ask_b();
+                turn(0, 0);
+                read_a(ta, 1);
+                if (more) commit_b();
+                oldest(more ? NS - 2 : 0);
+                turn(1, 0);
+            }
         }
         if (!late) tile_barrier();
     } else {
@@ -352,15 +453,100 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
             }
             read_b(tb, 0);
             read_a(ta, 0);
-            read_b(tb, 1);
+            if constexpr (NH == 2) read_b(tb, 1);
             mma(0, 0);
-            mma(0, 1);
+            if constexpr (NH == 2) mma(0, 1);
             read_a(ta, 1);
-            mma(1, 1);
+            if constexpr (NH == 2) mma(1, 1);
             mma(1, 0);
+            if (t + NS - 1 < total) commit_b();
             __builtin_amdgcn_s_waitcnt(kWaitLds);
         }
         tile_barrier();
+    }
+}
+
+// A tile's sums through LDS, so that memory is reached in whole pieces of rows instead of 4 values a lane of 16 rows
+// (256 x 256, two parts each way: 37 us a tile the one way, ROWS_NEW the other).  The tile goes by slices of rows as LDS
+// holds them; 4-float groups of a row stand at n ^ sum_place(row), which spreads writes by 16 rows, reads along rows
+// and reads of 8 columns by 64 rows over all banks.
+__device__ __forceinline__ int sum_place(int row) { return (row & 15) << 2 ^ (row >> 4 & 3) << 3; }
+
+template <typename S>
+struct SumSlices {
+    static constexpr int fit() {
+        for (int n = S::TM; n > 1; --n)
+            if (S::TM % n == 0 && n * 16 * S::WM * S::BN * 4 <= S::kLds * 2) return n;
+        return 1;
+    }
+    static constexpr int kTiles = fit(), kRows = kTiles * 16 * S::WM, kCount = S::TM / kTiles;
+    static_assert(kRows * S::BN * 4 <= S::kLds * 2 && S::BN % 64 == 0, "");
+    float* lds;
+    __device__ __forceinline__ explicit SumSlices(uint16_t* l) : lds(reinterpret_cast<float*>(l)) {}
+    // Row r of slice s is row row_of(s, r) of the tile.
+    __device__ __forceinline__ static int row_of(int s, int r) { return (r / (kTiles * 16)) * S::TM * 16 + s * kTiles * 16 + r % (kTiles * 16); }
+    __device__ __forceinline__ float* at(int r, int n) const { return lds + r * S::BN + (n ^ sum_place(r)); }   // n % 4 == 0
+    __device__ __forceinline__ float& one(int r, int n) const { return lds[r * S::BN + (n ^ sum_place(r))]; }
+    template <int SL>
+    __device__ __forceinline__ void put(const f32x4 (&acc)[S::TM][S::TN]) const {
+        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w / S::WN, wn = w % S::WN;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j)
+                *reinterpret_cast<f32x4*>(at((wm * kTiles + i) * 16 + (lane & 15), (wn * S::TN + j) * 16 + (lane >> 4) * 4)) =
+                    acc[SL * kTiles + i][j];
+        __syncthreads();
+    }
+    // 8 values of row r from column n on, for every 8 of the slice: ask(u, r, n) for what has to come from memory, then
+    // f(u, r, n, v), for a few of them at a time so that their loads are under way together.  What f leaves in v goes back
+    // if it says so.
+    static constexpr int kBatch = 4;
+    template <typename A, typename F>
+    __device__ __forceinline__ void rows8(A ask, F f) const {
+        constexpr int kPer = S::BN / 8, kAll = kRows * kPer;
+        for (int c0 = threadIdx.x; c0 < kAll; c0 += S::kThreads * kBatch) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int c = c0 + u * S::kThreads;
+                if (kAll % (S::kThreads * kBatch) == 0 || c < kAll) ask(u, c / kPer, c % kPer * 8);
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int c = c0 + u * S::kThreads;
+                if (kAll % (S::kThreads * kBatch) != 0 && c >= kAll) continue;
+                const int r = c / kPer, n = c % kPer * 8;
+                float v[8];
+                f32x4 *p = reinterpret_cast<f32x4*>(at(r, n)), *q = reinterpret_cast<f32x4*>(at(r, n + 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = (*p)[e], v[4 + e] = (*q)[e];
+                if (f(u, r, n, v)) {
+                    *p = f32x4{v[0], v[1], v[2], v[3]};
+                    *q = f32x4{v[4], v[5], v[6], v[7]};
+                }
+            }
+        }
+    }
+    // f(n, r, v): 8 values of column n from row r on, as they stand in LDS.
+    template <typename F>
+    __device__ __forceinline__ void columns8(F f) const {
+        constexpr int kPer = kRows / 8;
+        for (int c = threadIdx.x; c < S::BN * kPer; c += S::kThreads) {
+            const int n = c / kPer, r = c % kPer * 8;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = one(r + e, n);
+            f(n, r, v);
+        }
+    }
+};
+// f(slice number as a constant) for every slice.
+template <typename S, int I = 0, typename F>
+__device__ __forceinline__ void each_slice(F f) {
+    if constexpr (I < SumSlices<S>::kCount) {
+        f(std::integral_constant<int, I>());
+        each_slice<S, I + 1>(f);
     }
 }
 
