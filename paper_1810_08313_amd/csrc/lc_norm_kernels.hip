@@ -28,23 +28,48 @@ struct NormArgs {
     float eps, inv_cols;
 };
 
+// W consecutive elements as they stand in memory.
+template <typename T, int W>
+struct Raw {
+    typedef T V __attribute__((ext_vector_type(W)));
+    V v;
+    __device__ __forceinline__ void load(const T* p) { v = *reinterpret_cast<const V*>(p); }
+};
+template <typename T>
+struct Raw<T, 1> {
+    T v[1];
+    __device__ __forceinline__ void load(const T* p) { v[0] = *p; }
+};
+
 template <typename T, int W>
 struct Chunk;
 template <>
 struct Chunk<float, 1> {
     float v[1];
+    __device__ __forceinline__ void take(const Raw<float, 1>& r) {
+#pragma unroll
+        for (int e = 0; e < 1; ++e) v[e] = static_cast<float>(r.v[e]);
+    }
     __device__ __forceinline__ void load(const float* p) { v[0] = *p; }
     __device__ __forceinline__ void store(float* p) const { *p = v[0]; }
 };
 template <>
 struct Chunk<bf16_t, 1> {
     float v[1];
+    __device__ __forceinline__ void take(const Raw<bf16_t, 1>& r) {
+#pragma unroll
+        for (int e = 0; e < 1; ++e) v[e] = static_cast<float>(r.v[e]);
+    }
     __device__ __forceinline__ void load(const bf16_t* p) { v[0] = static_cast<float>(*p); }
     __device__ __forceinline__ void store(bf16_t* p) const { *p = static_cast<bf16_t>(v[0]); }
 };
 template <>
 struct Chunk<float, 4> {
     float v[4];
+    __device__ __forceinline__ void take(const Raw<float, 4>& r) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(r.v[e]);
+    }
     __device__ __forceinline__ void load(const float* p) {
         const f32x4 t = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll
@@ -55,6 +80,10 @@ struct Chunk<float, 4> {
 template <>
 struct Chunk<bf16_t, 8> {
     float v[8];
+    __device__ __forceinline__ void take(const Raw<bf16_t, 8>& r) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(r.v[e]);
+    }
     __device__ __forceinline__ void load(const bf16_t* p) {
         const bf16x8 t = *reinterpret_cast<const bf16x8*>(p);
 #pragma unroll
@@ -104,16 +133,23 @@ __global__ void __launch_bounds__(GROUP > kBlock ? GROUP : kBlock) norm_kernel(N
         gain[k] = a.gain && c < a.cols ? a.gain[i * a.param_rep + c] : 1.f;
         bias[k] = a.bias && c < a.cols ? a.bias[i * a.param_rep + c] : 0.f;
     }
-    for (int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / GROUP; row < a.rows; row += (int64_t)gridDim.x * kGroups) {
+    Raw<T, W> next[H];   // the next row, on its way while this one is summed up
+    auto ask = [&](int64_t row) {
+        if (row >= a.rows) return;
         const T* x = static_cast<const T*>(a.x) + i * a.x_rep + row * a.x_row;
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+            if ((h * GROUP + t) * W < a.cols) next[h].load(x + (h * GROUP + t) * W);
+    };
+    const int64_t stride = (int64_t)gridDim.x * kGroups, row0 = (int64_t)blockIdx.x * kGroups + threadIdx.x / GROUP;
+    ask(row0);
+    for (int64_t row = row0; row < a.rows; row += stride) {
         T* y = static_cast<T*>(a.y) + i * a.y_rep + row * a.y_row;
         Chunk<T, W> v[H];
         float s[1] = {0.f};
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-            const int c = (h * GROUP + t) * W;
-            if (c < a.cols) v[h].load(x + c);
-        }
+        for (int h = 0; h < H; ++h) v[h].take(next[h]);
+        ask(row + stride);
 #pragma unroll
         for (int h = 0; h < H; ++h)
             if ((h * GROUP + t) * W < a.cols)

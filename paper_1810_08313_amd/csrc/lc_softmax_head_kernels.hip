@@ -27,9 +27,8 @@ namespace lc {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kWide = 256;                        // classes of a workgroup of the first product: the parts of a row
 constexpr int64_t kKeepBytes = 2147483648LL;      // of e, and what stands beside it, at a time
-constexpr float kEScale = 32768.f;
+constexpr float kEScale = 32768.f, kEShift = 15.f;   // 2^15
 
 __device__ __forceinline__ uint16_t bits(bf16_t x) { return __builtin_bit_cast(uint16_t, x); }
 // x as the sum of three bf16 (24 bits: exact unless the last parts leave the exponent range).
@@ -102,11 +101,16 @@ __global__ void __launch_bounds__(kBlock) head_gather_kernel(GatherArgs g) {
     if (r0 >= kept) return;   // no product reads them
     const T* A = static_cast<const T*>(g.A) + i * g.a_rep;
     constexpr bool three = sizeof(T) == 4;
-#pragma unroll 4
+    int64_t row[16];
+    float val[16];
+#pragma unroll
+    for (int q = 0; q < 16; ++q) row[q] = g.order[i * g.order_rep + g.base + min(r0 + q * 4 + tr, kept - 1)];
+#pragma unroll
+    for (int q = 0; q < 16; ++q) val[q] = static_cast<float>(A[row[q] * g.a_row + min(c0 + tc, g.d - 1)]);
+#pragma unroll
     for (int q = 0; q < 16; ++q) {
         const int r = q * 4 + tr, c = c0 + tc;
-        float v = 0.f;
-        if (r0 + r < kept && c < g.d) v = static_cast<float>(A[g.order[i * g.order_rep + g.base + r0 + r] * g.a_row + c]);
+        const float v = r0 + r < kept && c < g.d ? val[q] : 0.f;
         tile[r][tc] = v;
         uint16_t p[3];
         split3(v, p);
@@ -137,9 +141,16 @@ __global__ void __launch_bounds__(kBlock) head_weights_kernel(const T* W, int64_
         const T* src = W + i * w_rep + r * w_row;
         uint16_t* to = out + ((int64_t)i * d + r) * cp;
         for (int c = (blockIdx.x * kBlock + threadIdx.x) * 8; c < cp; c += gridDim.x * kBlock * 8) {
+            T in[8];
+            if (c + 8 <= classes) {
+                __builtin_memcpy(in, src + c, sizeof(in));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) in[e] = c + e < classes ? src[c + e] : static_cast<T>(0.f);
+            }
             float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = c + e < classes ? static_cast<float>(src[c + e]) : 0.f;
+            for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(in[e]);
             s16x8 q[3];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -173,7 +184,6 @@ struct LogitArgs {
 
 template <typename S, typename E, BLayout LB>
 __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, LogitArgs l) {
-    static_assert(S::BN == kWide, "a row's part is a workgroup's");
     __shared__ __align__(1024) uint16_t lds[S::kLds];
     const TilePlace pl = tile_place<S>(a);
     if (pl.batch < 0) return;
@@ -182,25 +192,32 @@ __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, Lo
     f32x4 acc[S::TM][S::TN];
     tile_sums<bf16_t, S, LB>(a, pl, 0, a.K / S::BK, lds, acc);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w / S::WN, wn = w % S::WN;
-    const int nw = pl.tn * S::BN + wn * S::TN * 16 + (lane >> 4) * 4;
+    const int first = pl.tn * S::BN + wn * S::TN * 16, nw = first + (lane >> 4) * 4;   // the wavefront's classes, the lane's
     const float* bias = l.bias ? l.bias + pl.batch * l.bias_rep : nullptr;
     float* red = reinterpret_cast<float*>(lds);   // [2][WN][BM], free since the last product's barrier
-    // bias, classes that do not exist, the row's maximum over the wavefront's 64 classes
+    const bool whole = pl.tn * S::BN + S::BN <= l.classes;
+    // bias, classes that do not exist, the row's maximum over the wavefront's classes
     float top[S::TM];
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) top[i] = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j)
+    for (int j = 0; j < S::TN; ++j) {
+        float b[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int n = nw + j * 16 + e;
-            const float b = bias && n < l.classes ? bias[n] : 0.f;
+            b[e] = bias ? bias[whole ? n : min(n, l.classes - 1)] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool none = !whole && nw + j * 16 + e >= l.classes;
 #pragma unroll
             for (int i = 0; i < S::TM; ++i) {
-                acc[i][j][e] = n < l.classes ? acc[i][j][e] + b : -INFINITY;
+                acc[i][j][e] = none ? -INFINITY : acc[i][j][e] + b[e];
                 top[i] = fmaxf(top[i], acc[i][j][e]);
             }
         }
+    }
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) {
         top[i] = fmaxf(top[i], __shfl_xor(top[i], 16));
@@ -208,6 +225,8 @@ __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, Lo
         if (lane < 16) red[wn * S::BM + (wm * S::TM + i) * 16 + lane] = top[i];
     }
     __syncthreads();
+    // e = 2^(z log2(e) - top log2(e)), times 2^15 where it is kept as fp16: one multiply-add and one exponential a logit
+    constexpr float kLog2e = 1.44269504f, kShift = sizeof(E) == 2 ? kEShift : 0.f;
     float sum[S::TM];
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) {
@@ -219,15 +238,25 @@ __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, Lo
         const float ref = t == -INFINITY ? 0.f : t;   // a part without a class left: e = 0, not NaN
         const int y = m < kept ? l.label[pl.batch * l.label_rep + l.base + m] : -1;
         float s = 0.f;
+        const bool mine = __any(y >= first && y < first + S::TN * 16);   // a row's label is among the wavefront's classes
 #pragma unroll
         for (int j = 0; j < S::TN; ++j) {
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float z = acc[i][j][e];
-                v[e] = __expf(z - ref);
-                if (nw + j * 16 + e == y) l.z_label[(int64_t)pl.batch * l.n + m] = z;
-                else s += v[e];
+                v[e] = __builtin_amdgcn_exp2f(fmaf(z - ref, kLog2e, kShift));
+            }
+            if (mine) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool is = nw + j * 16 + e == y;
+                    if (is) l.z_label[(int64_t)pl.batch * l.n + m] = acc[i][j][e];
+                    s += is ? 0.f : v[e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s += v[e];
             }
             const int n = nw + j * 16;
             if (l.e && m < kept && n < l.ep) {
@@ -237,7 +266,7 @@ __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, Lo
                 } else {
                     f16x4 h;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) h[e] = static_cast<f16_t>(v[e] * kEScale);
+                    for (int e = 0; e < 4; ++e) h[e] = static_cast<f16_t>(v[e]);
                     *reinterpret_cast<f16x4*>(to) = h;
                 }
             }
@@ -255,7 +284,7 @@ __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, Lo
             float s = sum[i];
 #pragma unroll
             for (int k = 1; k < S::WN; ++k) s += red[(S::WN + k) * S::BM + r];
-            if (m < kept) l.stat[((int64_t)pl.batch * l.n + m) * l.parts + pl.tn] = make_float2(top[i], s);
+            if (m < kept) l.stat[((int64_t)pl.batch * l.n + m) * l.parts + pl.tn] = make_float2(top[i], sizeof(E) == 2 ? s * (1.f / kEScale) : s);
         }
     }
 }
@@ -310,7 +339,7 @@ struct DeltaArgs {
     const int32_t* label;
     const int* kept;
     int64_t label_rep;
-    int base, n, parts, classes, row_blocks, block_rows;
+    int base, n, parts, wide, classes, row_blocks, block_rows;
     float* db_part;              // [m][row_blocks][ep]
 };
 
@@ -339,7 +368,7 @@ __global__ void __launch_bounds__(kBlock) head_delta_kernel(DeltaArgs d) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] = static_cast<float>(p[k]);
                 }
-                const float f = d.coef[((int64_t)i * d.n + r) * d.parts + c / kWide];
+                const float f = d.coef[((int64_t)i * d.n + r) * d.parts + c / d.wide];
                 const int y = d.label[i * d.label_rep + d.base + r] - c;
                 const float dy = d.delta_label[(int64_t)i * d.n + r];
 #pragma unroll
@@ -506,12 +535,14 @@ __global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across
 // Tiles of the products: one part (bf16 operands) or three (fp32).
 template <bool THREE>
 struct Tiles {
+    typedef TileShape<64, 128, 1, 4, 64, 1, 3> Few;
     typedef TileShape<64, 256, 1, 4, 64, 1, 2> Rows64;
     typedef TileShape<128, 256, 2, 4, 64, 1, 3> Rows128;
     typedef TileShape<256, 256, 2, 4, 64, 1, 2> Rows256;
 };
 template <>
 struct Tiles<true> {
+    typedef TileShape<64, 128, 1, 4, 32, 3, 2> Few;
     typedef TileShape<64, 256, 1, 4, 32, 3, 2> Rows64;
     typedef TileShape<128, 256, 2, 4, 32, 3, 2> Rows128;
     typedef Rows128 Rows256;   // 256 x 256 in three parts would take 192 KB of LDS for two buffers
@@ -530,12 +561,16 @@ void with_tile(TileArgs& a, F f) {
     else go(typename Tiles<THREE>::Rows256());
 }
 
+// Classes of a workgroup of the first product: 256, and 128 where up to 64 rows and 256 classes would leave compute units
+// without work (one row, 2048 x 32000: 125 workgroups, 44 us; 250: 33).
+int head_wide(const lc_head_args& h, bool) { return h.rows <= 64 && (int64_t)h.m * ((h.classes + 255) / 256) < 256 ? 128 : 256; }
+
 struct HeadPlan {
     bool grad, three, copy_w, any_w;   // gradients; fp32 operands in three parts; W copied first, or of any alignment
     int d, dp, d4, cp, parts;    // inputs and padded, classes of a row of the copy of W, parts of a row's sum
     int64_t ep;                  // classes of a row of e
     int chunk, group, splits;    // rows and replicas at a time, shares of dA's product
-    int block_rows;
+    int block_rows, wide;        // classes of a workgroup of the first product, the parts of a row
     int32_t *order, *label;
     int* kept;
     float *row_loss, *z_label, *coef, *delta_label, *da, *db_part, *db_acc, *dw_acc, *e32;
@@ -575,7 +610,8 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
     p.d = h.inputs;
     p.dp = static_cast<int>(round_up(h.inputs, kPadK));
     p.d4 = static_cast<int>(round_up(h.inputs, 4));
-    p.parts = static_cast<int>((h.classes + kWide - 1) / kWide);
+    p.wide = head_wide(h, p.three);
+    p.parts = static_cast<int>((h.classes + p.wide - 1) / p.wide);
     p.ep = round_up(h.classes, kPadK);
     // bf16 weights are read where they stand: straight into LDS if every row starts on 16 bytes and holds whole chunks of 8,
     // through registers otherwise (8 x 128 rows, 512 x 50257: a copy first cost 207 us of 860)
@@ -609,8 +645,8 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
         auto count = [&](auto) { tiles = (int64_t)t.per_batch * g; };
         if (p.three) with_tile<true>(t, count);
         else with_tile<false>(t, count);
-        // few tiles: the classes are shared out until every compute unit has a share, of 256 at least
-        p.splits = static_cast<int>(std::max<int64_t>(1, std::min((256 + tiles - 1) / tiles, p.ep / (4 * kPadK))));
+        // few tiles: the classes are shared out until every compute unit has a share, of 128 at least
+        p.splits = static_cast<int>(std::max<int64_t>(1, std::min((256 + tiles - 1) / tiles, p.ep / (2 * kPadK))));
         p.coef = c.take<float>(g * n * p.parts);
         p.delta_label = c.take<float>(g * n);
         p.at = c.take<uint16_t>(np * g * p.d * n);
@@ -674,7 +710,7 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
                               h.classes, p.parts, p.stat, p.z_label, p.grad ? (p.three ? (void*)p.e32 : (void*)p.dz) : nullptr, p.ep};
             typedef typename std::conditional<sizeof(T) == 4, float, f16_t>::type E;
             if (here) {
-                with_tile<sizeof(T) == 4>(t, [&](auto s) {
+                auto logits = [&](auto s) {
                     typedef decltype(s) S;
                     if constexpr (sizeof(T) == 2) {
                         if (p.any_w) {
@@ -683,13 +719,15 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
                         }
                     }
                     head_logits_kernel<S, E, NMajor><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, l);
-                });
+                };
+                if (p.wide == 128) logits(typename Tiles<sizeof(T) == 4>::Few());
+                else with_tile<sizeof(T) == 4>(t, logits);
                 head_join_kernel<<<dim3((here + 3) / 4, g), kBlock, 0, st>>>(l, order, p.three ? 1.f : 1.f / kEScale, p.coef,
                                                                             p.delta_label, row_loss + g0 * loss_rep, loss_rep);
             }
             if (!p.grad) continue;
             const int row_blocks = static_cast<int>(round_up(here, 64)) / p.block_rows;
-            const DeltaArgs da{l.e, p.dz, p.ep, dz_part, p.coef, p.delta_label, label, kept, rows, base, static_cast<int>(n), p.parts,
+            const DeltaArgs da{l.e, p.dz, p.ep, dz_part, p.coef, p.delta_label, label, kept, rows, base, static_cast<int>(n), p.parts, p.wide,
                                h.classes, row_blocks, p.block_rows, p.db_part};
             if (here) head_delta_kernel<E><<<dim3(static_cast<unsigned>((p.ep + kBlock * 8 - 1) / (kBlock * 8)), row_blocks, g), kBlock, 0, st>>>(da);
             Across x{k == 0, k + 1 == chunks, p.db_acc, kept};

