@@ -536,6 +536,7 @@ __global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across
 template <bool THREE>
 struct Tiles {
     typedef TileShape<64, 128, 1, 4, 64, 1, 3> Few;
+    typedef TileShape<128, 128, 2, 2, 64, 1, 2> Half;
     typedef TileShape<64, 256, 1, 4, 64, 1, 2> Rows64;
     typedef TileShape<128, 256, 2, 4, 64, 1, 3> Rows128;
     typedef TileShape<256, 256, 2, 4, 64, 1, 2> Rows256;
@@ -543,6 +544,7 @@ struct Tiles {
 template <>
 struct Tiles<true> {
     typedef TileShape<64, 128, 1, 4, 32, 3, 2> Few;
+    typedef TileShape<128, 128, 2, 2, 32, 3, 2> Half;
     typedef TileShape<64, 256, 1, 4, 32, 3, 2> Rows64;
     typedef TileShape<128, 256, 2, 4, 32, 3, 2> Rows128;
     typedef Rows128 Rows256;   // 256 x 256 in three parts would take 192 KB of LDS for two buffers
@@ -561,9 +563,13 @@ void with_tile(TileArgs& a, F f) {
     else go(typename Tiles<THREE>::Rows256());
 }
 
-// Classes of a workgroup of the first product: 256, and 128 where up to 64 rows and 256 classes would leave compute units
-// without work (one row, 2048 x 32000: 125 workgroups, 44 us; 250: 33).
-int head_wide(const lc_head_args& h, bool) { return h.rows <= 64 && (int64_t)h.m * ((h.classes + 255) / 256) < 256 ? 128 : 256; }
+// Classes of a workgroup of the first product: 256; 128 where up to 64 rows and 256 classes would leave compute units
+// without work (one row, 2048 x 32000: 125 workgroups, 44 us; 250: 33), and for 65 to 128 rows, so that two workgroups share
+// a compute unit (8 x 128 rows, 512 x 50257: 228 and 196 us, 50304: 180 and 167).
+int head_wide(const lc_head_args& h) {
+    if (h.rows > 128) return 256;
+    return h.rows > 64 || (int64_t)h.m * ((h.classes + 255) / 256) < 256 ? 128 : 256;
+}
 
 struct HeadPlan {
     bool grad, three, copy_w, any_w;   // gradients; fp32 operands in three parts; W copied first, or of any alignment
@@ -610,7 +616,7 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
     p.d = h.inputs;
     p.dp = static_cast<int>(round_up(h.inputs, kPadK));
     p.d4 = static_cast<int>(round_up(h.inputs, 4));
-    p.wide = head_wide(h, p.three);
+    p.wide = head_wide(h);
     p.parts = static_cast<int>((h.classes + p.wide - 1) / p.wide);
     p.ep = round_up(h.classes, kPadK);
     // bf16 weights are read where they stand: straight into LDS if every row starts on 16 bytes and holds whole chunks of 8,
@@ -720,7 +726,8 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
                     }
                     head_logits_kernel<S, E, NMajor><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, l);
                 };
-                if (p.wide == 128) logits(typename Tiles<sizeof(T) == 4>::Few());
+                if (p.wide == 128 && rows <= 64) logits(typename Tiles<sizeof(T) == 4>::Few());
+                else if (p.wide == 128) logits(typename Tiles<sizeof(T) == 4>::Half());
                 else with_tile<sizeof(T) == 4>(t, logits);
                 head_join_kernel<<<dim3((here + 3) / 4, g), kBlock, 0, st>>>(l, order, p.three ? 1.f : 1.f / kEScale, p.coef,
                                                                             p.delta_label, row_loss + g0 * loss_rep, loss_rep);
