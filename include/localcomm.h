@@ -471,10 +471,9 @@ typedef struct {
 int lc_layer_norm(int m, int64_t rows, int32_t cols, int dtype, lc_rows x, const float* gain, const float* bias,
                   int64_t param_replica, float eps, lc_rows y, float* stats, void* stream);
 
-/* Its backward pass from x, dy and stats: dx (which may stand where x or dy does, not where neither
- * of them but part of one does), and the sums over the rows dgain = sum dy * (x - mean) * r and dbias =
- * sum dy, device fp32 [cols] per replica, grad_replica floats apart; NULL: not formed.  They are
- * written, not added to; rows = 0 gives zeros.  The workspace (device, 256-byte aligned) is needed for
+/* Its backward pass from x, dy and stats: dx, which may stand exactly where x or dy does, and the sums
+ * over the rows dgain = sum dy * (x - mean) * r and dbias = sum dy, device fp32 [cols] per replica,
+ * grad_replica floats apart; NULL: not formed.  They are written, not added to; rows = 0 gives zeros.  The workspace (device, 256-byte aligned) is needed for
  * the sums only.  Errors: as above, LC_ERR_WORKSPACE. */
 size_t lc_layer_norm_workspace_bytes(int m, int64_t rows, int32_t cols);
 int lc_layer_norm_grad(int m, int64_t rows, int32_t cols, int dtype, lc_rows x, lc_rows dy, const float* gain,
@@ -519,7 +518,7 @@ typedef struct {
  * in chunks so that what is kept for a chunk stays near 2 GB. */
 size_t lc_softmax_head_workspace_bytes(const lc_head_args* args, int with_grad);
 /* loss (and row_loss); and loss with dA, dW and db.  Outputs are written, not added to, and overlap no
- * input.  Errors: LC_ERR_ARG, LC_ERR_ALIGN (elements; workspace 256 bytes), LC_ERR_UNSUPPORTED (beyond the sizes
+ * input (a gradient that starts where an input does is refused).  Errors: LC_ERR_ARG, LC_ERR_ALIGN (elements; workspace 256 bytes), LC_ERR_UNSUPPORTED (beyond the sizes
  * above), LC_ERR_WORKSPACE, LC_ERR_HIP. */
 int lc_softmax_head_loss(const lc_head_args* args, void* workspace, size_t workspace_bytes, void* stream);
 int lc_softmax_head_grad(const lc_head_args* args, void* workspace, size_t workspace_bytes, void* stream);

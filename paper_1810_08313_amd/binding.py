@@ -300,9 +300,13 @@ def _first(where: str, t, stream):
     return stream, not here or stream != torch.cuda.current_stream(t.device)
 
 
-def _on(stream):
-    """Context in which what is allocated belongs to the stream that the call runs on."""
+def _on(stream, *tensors):
+    """Context in which what is allocated belongs to the stream that the call runs on; the tensors, which may belong to
+    another, are not given away before it is through with them."""
     import torch
+    for t in tensors:
+        if t is not None and t.device == stream.device:
+            t.record_stream(stream)
     return torch.cuda.stream(stream)   # of its device, too
 
 
@@ -344,7 +348,7 @@ def layer_norm(x, gain=None, bias=None, eps: float = 1e-5, out=None, stream=None
     where = "lc_layer_norm"
     stream, other = _first(where, x, stream)
     if other:
-        with _on(stream):
+        with _on(stream, x, gain, bias, out):
             return layer_norm(x, gain, bias, eps, out)
     f32, t, dev, shape = torch.float32, x.dtype, x.device, x.shape
     m, rows, cols = shape
@@ -367,13 +371,17 @@ def layer_norm_grad(x, dy, gain, stats, dx=None, dgain=None, dbias=None, stream=
     where = "lc_layer_norm_grad"
     stream, other = _first(where, x, stream)
     if other:
-        with _on(stream):
+        with _on(stream, x, dy, gain, stats, dx, dgain, dbias):
             return layer_norm_grad(x, dy, gain, stats, dx, dgain, dbias)
     f32, t, dev, shape = torch.float32, x.dtype, x.device, x.shape
     m, rows, cols = shape
     dx = torch.empty(shape, dtype=t, device=dev) if dx is None else dx
-    dgain = torch.empty((m, cols), dtype=f32, device=dev) if dgain is None else dgain
-    dbias = torch.empty((m, cols), dtype=f32, device=dev) if dbias is None else dbias
+    if dgain is None and dbias is None:
+        dgain, dbias = torch.empty((2, m, cols), dtype=f32, device=dev).unbind(0)
+    elif dgain is None:
+        dgain = torch.empty_like(dbias)
+    elif dbias is None:
+        dbias = torch.empty_like(dgain)
     _check(where, "stats", stats, (m, rows, 2), f32, dev)
     if not stats.is_contiguous():
         _refuse(where, "stats is not contiguous")
@@ -437,7 +445,7 @@ def softmax_head_loss(A, W, bias, labels, stream=None):
     where = "lc_softmax_head_loss"
     stream, other = _first(where, A, stream)
     if other:
-        with _on(stream):
+        with _on(stream, A, W, bias, labels):
             return _softmax_head(where, A, W, bias, labels, stream, None)
     return _softmax_head(where, A, W, bias, labels, stream, None)
 
@@ -447,7 +455,7 @@ def softmax_head_grad(A, W, bias, labels, dA=None, dW=None, db=None, grad_dtype=
     where = "lc_softmax_head_grad"
     stream, other = _first(where, A, stream)
     if other:
-        with _on(stream):
+        with _on(stream, A, W, bias, labels, dA, dW, db):
             return _softmax_head(where, A, W, bias, labels, stream, (dA, dW, db, grad_dtype))
     return _softmax_head(where, A, W, bias, labels, stream, (dA, dW, db, grad_dtype))
 
@@ -458,7 +466,7 @@ def orthogonalize(src, steps: int = 5, out=None, stream=None):
     where = "lc_orthogonalize"
     stream, other = _first(where, src, stream)
     if other:
-        with _on(stream):
+        with _on(stream, src, out):
             return orthogonalize(src, steps, out)
     t, dev, shape = src.dtype, src.device, src.shape
     m, rows, cols = shape
@@ -479,7 +487,7 @@ def update_orthogonal(X, V, G, lr: float, beta: float, wd: float = 0.0, steps: i
     where = "lc_update_orthogonal"
     stream, other = _first(where, X, stream)
     if other:
-        with _on(stream):
+        with _on(stream, X, V, G):
             return update_orthogonal(X, V, G, lr, beta, wd, steps)
     f32, dev, shape = torch.float32, X.device, X.shape
     m, rows, cols = shape

@@ -4,7 +4,7 @@
 //   dZ = softmax(Z) - onehot(y),  dA = dZ W^T / kept,  dW = A^T dZ / kept,  db = sum_rows dZ / kept
 //
 // Bound by three products of rows x inputs x classes where the batch is long, by reading W twice and writing dW
-// once where it is short.  Z itself never reaches memory: the product's workgroup, 256 classes wide, reduces its
+// once where it is short.  Z itself never reaches memory: the product's workgroup, 128 or 256 classes wide, reduces its
 // part of a row to a maximum and a sum of exponentials, and the parts of a row are joined afterwards.  For the
 // gradient it leaves e = exp(z - the part's maximum), for as many rows at a time as 2 GB hold; with the joined sum a
 // second pass turns e into dZ in place (and sums its columns, db), which the two gradient products read.  Leaving e
@@ -16,8 +16,8 @@
 //
 // bf16 operands: e is kept as fp16 times 2^15 (11 bits down to 2^-29 of the part's maximum), dZ rounded to bf16
 // once and divided by the number of rows behind the sums (so that the label's -1 stays exact: 1 / kept would be off by
-// up to 2^-9 in every row, the same way), sums in 32 bits.  The label's own delta is -(sum of the others) / (whole sum), formed in 32 bits: p - 1 would
-// keep no digits of a well-fitted row.
+// up to 2^-9 in every row, the same way), sums in 32 bits.  The label's own delta is -(sum of the others) / (whole
+// sum), formed in 32 bits: p - 1 would keep no digits of a well-fitted row.
 // fp32 operands: the exact sum of three bf16 parts each, six of the nine part products (what is left out is below
 // 2^-24 of |a| |b|), e and dZ in 32 bits.
 #include "lc_operators.h"
@@ -605,6 +605,7 @@ int head_check(const lc_head_args* h, bool grad) {
     if (rc == LC_OK) rc = check_output(h->dW, h->m, h->inputs, h->classes, h->grad_dtype);
     if (rc != LC_OK) return rc;
     if (h->db && h->m > 1 && h->db_replica < h->classes) return LC_ERR_ARG;
+    if (h->dW.p == h->W.p || (h->rows > 0 && h->dA.p == h->A.p)) return LC_ERR_ARG;   // what later chunks still read
     if (!aligned_to(h->db, element_bytes(h->grad_dtype))) return LC_ERR_ALIGN;
     return LC_OK;
 }

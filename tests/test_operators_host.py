@@ -43,7 +43,7 @@ def head_args(**kw):
     from paper_1810_08313_amd.binding import LcHeadArgs
     h = LcHeadArgs(m=2, inputs=64, rows=8, classes=1000, dtype=1, grad_dtype=1, A=R(row=64, replica=512), W=R(row=1000, replica=64000),
                    bias=P, bias_replica=1000, labels=P, label_replica=8, loss=P, row_loss=P, row_loss_replica=8,
-                   dA=R(row=64, replica=512), dW=R(row=1000, replica=64000), db=P, db_replica=1000)
+                   dA=R(2 * P, row=64, replica=512), dW=R(3 * P, row=1000, replica=64000), db=P, db_replica=1000)
     for k, v in kw.items():
         setattr(h, k, v)
     return h
@@ -57,7 +57,8 @@ BAD_HEADS = [
     (dict(inputs=(1 << 20) + 1), -8),
 ]
 BAD_GRADS = [
-    (dict(grad_dtype=3), -1), (dict(dA=R(None)), -1), (dict(dW=R(None)), -1), (dict(dA=R(row=64, replica=0)), -1),
+    (dict(dA=R(row=64, replica=512)), -1), (dict(dW=R(row=1000, replica=64000)), -1),   # where A and W stand
+    (dict(grad_dtype=3), -1), (dict(dA=R(None)), -1), (dict(dW=R(None)), -1), (dict(dA=R(2 * P, row=64, replica=0)), -1),
     (dict(dW=R(row=1000, replica=0)), -1), (dict(db_replica=999), -1), (dict(db=P + 1), -4),
 ]
 
@@ -86,7 +87,7 @@ def test_softmax_head_workspace_stays_bounded(L, rows, d, classes, dtype):
     """A whole batch's logits are never kept: beyond what a chunk of rows needs there are only copies of the operands."""
     e = 2 if dtype else 4
     h = head_args(m=1, rows=rows, inputs=d, classes=classes, dtype=dtype, grad_dtype=dtype, A=R(row=d), W=R(row=classes),
-                  dA=R(row=d), dW=R(row=classes), db=P)
+                  dA=R(2 * P, row=d), dW=R(3 * P, row=classes), db=P)
     n = L.lc_softmax_head_workspace_bytes(C.byref(h), 1)
     chunk = min(rows + 64, 65536)
     kept = max(2 << 30, 256 * (classes + 64) * 10) * 1.1
