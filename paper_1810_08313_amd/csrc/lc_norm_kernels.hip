@@ -233,21 +233,36 @@ __global__ void __launch_bounds__(GROUP > kBlock ? GROUP : kBlock) norm_grad_ker
         gain[k] = a.gain && c < a.cols ? a.gain[i * a.param_rep + c] : 1.f;
         dg[k] = db[k] = 0.f;
     }
-    for (int64_t row = (int64_t)blockIdx.x * kGroups + group; row < a.rows; row += (int64_t)gridDim.x * kGroups) {
+    Raw<T, W> next_x[H], next_dy[H];   // the next row
+    float next_mean = 0.f, next_r = 0.f;
+    auto ask = [&](int64_t row) {
+        if (row >= a.rows) return;
         const T* x = static_cast<const T*>(a.x) + i * a.x_rep + row * a.x_row;
         const T* dy = static_cast<const T*>(a.dy) + i * a.dy_rep + row * a.dy_row;
-        T* dx = static_cast<T*>(a.y) + i * a.y_rep + row * a.y_row;
-        Chunk<T, W> n[H], h[H];
         const float* st = a.stats + ((int64_t)i * a.rows + row) * 2;
-        const float mean = st[0], r = st[1];
+        next_mean = st[0];
+        next_r = st[1];
 #pragma unroll
         for (int k = 0; k < H; ++k) {
             const int c = (k * GROUP + t) * W;
             if (c < a.cols) {
-                n[k].load(x + c);
-                h[k].load(dy + c);
+                next_x[k].load(x + c);
+                next_dy[k].load(dy + c);
             }
         }
+    };
+    const int64_t stride = (int64_t)gridDim.x * kGroups, row0 = (int64_t)blockIdx.x * kGroups + group;
+    ask(row0);
+    for (int64_t row = row0; row < a.rows; row += stride) {
+        T* dx = static_cast<T*>(a.y) + i * a.y_rep + row * a.y_row;
+        Chunk<T, W> n[H], h[H];
+        const float mean = next_mean, r = next_r;
+#pragma unroll
+        for (int k = 0; k < H; ++k) {
+            n[k].take(next_x[k]);
+            h[k].take(next_dy[k]);
+        }
+        ask(row + stride);
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < H; ++k)
@@ -347,19 +362,29 @@ __global__ void __launch_bounds__(kBlock) norm_columns_kernel(NormArgs a) {
     out[a.cols + c] = b;
 }
 
-// The partial rows added up: 64 columns per workgroup, 4 wavefronts each a quarter of the rows.
-__global__ void __launch_bounds__(kBlock) norm_reduce_kernel(const float* partial, int blocks, int cols, float* dgain, float* dbias,
-                                                             int64_t grad_rep) {
-    __shared__ float s[4][64];
-    const int i = blockIdx.y, which = blockIdx.z, w = threadIdx.x >> 6, c = blockIdx.x * 64 + (threadIdx.x & 63);
+// The partial rows added up: 64 columns per workgroup, 16 wavefronts each a sixteenth of the rows (of 256 rows x 2048
+// columns x 4 replicas: 17 us with 4 wavefronts that wait for every row, 5 so).
+constexpr int kReduceWaves = 16;
+__global__ void __launch_bounds__(64 * kReduceWaves) norm_reduce_kernel(const float* partial, int blocks, int cols, float* dgain, float* dbias,
+                                                                        int64_t grad_rep) {
+    __shared__ float s[kReduceWaves][64];
+    const int i = blockIdx.y, which = blockIdx.z, w = threadIdx.x >> 6, t = threadIdx.x & 63, c = blockIdx.x * 64 + t;
     float* out = which ? dbias : dgain;
     if (!out) return;
     float v = 0.f;
-    if (c < cols)
-        for (int b = w; b < blocks; b += 4) v += partial[((int64_t)i * blocks + b) * 2 * cols + (int64_t)which * cols + c];
-    s[w][threadIdx.x & 63] = v;
+    if (c < cols) {
+        const float* p = partial + (int64_t)i * blocks * 2 * cols + (int64_t)which * cols + c;
+#pragma unroll 8
+        for (int b = w; b < blocks; b += kReduceWaves) v += p[(int64_t)b * 2 * cols];
+    }
+    s[w][t] = v;
     __syncthreads();
-    if (w == 0 && c < cols) out[i * grad_rep + c] = (s[0][threadIdx.x] + s[1][threadIdx.x]) + (s[2][threadIdx.x] + s[3][threadIdx.x]);
+    if (w == 0 && c < cols) {
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < kReduceWaves; ++k) sum += s[k][t];
+        out[i * grad_rep + c] = sum;
+    }
 }
 
 // Workgroups that a replica's rows are shared out to: the whole chip several times over with all replicas
@@ -457,7 +482,7 @@ int lc_layer_norm_grad(int m, int64_t rows, int32_t cols, int dtype, lc_rows x, 
         if (dtype == LC_GEMM_BF16) vec ? launch_norm_grad<bf16_t, 8>(a, m, st) : launch_norm_grad<bf16_t, 1>(a, m, st);
         else vec ? launch_norm_grad<float, 4>(a, m, st) : launch_norm_grad<float, 1>(a, m, st);
     }
-    if (sums) norm_reduce_kernel<<<dim3((cols + 63) / 64, m, 2), kBlock, 0, st>>>(a.partial, a.blocks, cols, dgain, dbias, grad_replica);
+    if (sums) norm_reduce_kernel<<<dim3((cols + 63) / 64, m, 2), 64 * kReduceWaves, 0, st>>>(a.partial, a.blocks, cols, dgain, dbias, grad_replica);
     return hipGetLastError() == hipSuccess ? LC_OK : LC_ERR_HIP;
 }
 
