@@ -336,9 +336,15 @@ def _vector(where, name, t, shape, dtype, device):
     return t.data_ptr(), _check(where, name, t, shape, dtype, device)[0]
 
 
-def _workspace(n: int, device):
+def _like(x):
+    """A contiguous tensor of the shape of x (half the time of torch.empty with everything spelled out)."""
     import torch
-    return torch.empty(n or 1, dtype=torch.uint8, device=device)
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
+def _workspace(n: int, like):
+    import torch
+    return like.new_empty(n or 1, dtype=torch.uint8)
 
 
 def layer_norm(x, gain=None, bias=None, eps: float = 1e-5, out=None, stream=None):
@@ -352,8 +358,8 @@ def layer_norm(x, gain=None, bias=None, eps: float = 1e-5, out=None, stream=None
             return layer_norm(x, gain, bias, eps, out)
     f32, t, dev, shape = torch.float32, x.dtype, x.device, x.shape
     m, rows, cols = shape
-    y = torch.empty(shape, dtype=t, device=dev) if out is None else out
-    stats = torch.empty((m, rows, 2), dtype=f32, device=dev)
+    y = _like(x) if out is None else out
+    stats = x.new_empty((m, rows, 2), dtype=f32)
     gp, gs = _vector(where, "gain", gain, (m, cols), f32, dev)
     bp, bs = _vector(where, "bias", bias, (m, cols), f32, dev)
     if gs != bs and gp and bp and m > 1:
@@ -375,9 +381,9 @@ def layer_norm_grad(x, dy, gain, stats, dx=None, dgain=None, dbias=None, stream=
             return layer_norm_grad(x, dy, gain, stats, dx, dgain, dbias)
     f32, t, dev, shape = torch.float32, x.dtype, x.device, x.shape
     m, rows, cols = shape
-    dx = torch.empty(shape, dtype=t, device=dev) if dx is None else dx
+    dx = _like(x) if dx is None else dx
     if dgain is None and dbias is None:
-        dgain, dbias = torch.empty((2, m, cols), dtype=f32, device=dev).unbind(0)
+        dgain, dbias = x.new_empty((2, m, cols), dtype=f32).unbind(0)
     elif dgain is None:
         dgain = torch.empty_like(dbias)
     elif dbias is None:
@@ -392,7 +398,7 @@ def layer_norm_grad(x, dy, gain, stats, dx=None, dgain=None, dbias=None, stream=
         _refuse(where, "dgain and dbias have different distances between replicas")
     L = lib()
     n = L.lc_layer_norm_workspace_bytes(m, rows, cols)
-    ws = _workspace(n, dev)
+    ws = _workspace(n, x)
     rc = L.lc_layer_norm_grad(m, rows, cols, t is torch.bfloat16, _rows(where, "x", x, shape, t, dev), _rows(where, "dy", dy, shape, t, dev),
                               gp, gs, stats.data_ptr(), _rows(where, "dx", dx, shape, t, dev), dgp, dbp, dgs, ws.data_ptr(), n,
                               stream.cuda_stream)
@@ -412,11 +418,11 @@ def _softmax_head(where, A, W, bias, labels, stream, grads):
     h.A, h.W = _rows(where, "A", A, A.shape, t, dev), _rows(where, "W", W, (m, d, classes), t, dev)
     h.bias, h.bias_replica = _vector(where, "bias", bias, (m, classes), f32, dev)
     h.labels, h.label_replica = _vector(where, "labels", labels, (m, rows), torch.int32, dev)
-    loss = torch.empty(m, dtype=f32, device=dev)
+    loss = A.new_empty(m, dtype=f32)
     h.loss = loss.data_ptr()
     L = lib()
     if grads is None:
-        row_loss = torch.empty((m, rows), dtype=f32, device=dev)
+        row_loss = A.new_empty((m, rows), dtype=f32)
         h.row_loss, h.row_loss_replica = row_loss.data_ptr(), rows
         out, fn = (loss, row_loss), L.lc_softmax_head_loss
     else:
@@ -424,15 +430,15 @@ def _softmax_head(where, A, W, bias, labels, stream, grads):
         dtype = dtype or (dW.dtype if dW is not None else t)
         if dtype is not f32 and dtype is not torch.bfloat16:
             _refuse(where, f"gradients of element type {dtype}")
-        dA = torch.empty((m, rows, d), dtype=t, device=dev) if dA is None else dA
-        dW = torch.empty((m, d, classes), dtype=dtype, device=dev) if dW is None else dW
-        db = torch.empty((m, classes), dtype=dtype, device=dev) if db is None else db
+        dA = _like(A) if dA is None else dA
+        dW = A.new_empty((m, d, classes), dtype=dtype) if dW is None else dW
+        db = A.new_empty((m, classes), dtype=dtype) if db is None else db
         h.grad_dtype = dtype is torch.bfloat16
         h.dA, h.dW = _rows(where, "dA", dA, A.shape, t, dev), _rows(where, "dW", dW, (m, d, classes), dtype, dev)
         h.db, h.db_replica = _vector(where, "db", db, (m, classes), dtype, dev)
         out, fn = (loss, dA, dW, db), L.lc_softmax_head_grad
     n = L.lc_softmax_head_workspace_bytes(C.byref(h), grads is not None)
-    ws = _workspace(n, dev)
+    ws = _workspace(n, A)
     rc = fn(C.byref(h), ws.data_ptr(), n, stream.cuda_stream)
     if rc:
         raise LcError(rc, where)
@@ -470,10 +476,10 @@ def orthogonalize(src, steps: int = 5, out=None, stream=None):
             return orthogonalize(src, steps, out)
     t, dev, shape = src.dtype, src.device, src.shape
     m, rows, cols = shape
-    out = torch.empty(shape, dtype=t, device=dev) if out is None else out
+    out = _like(src) if out is None else out
     L = lib()
     n = L.lc_orthogonal_workspace_bytes(m, rows, cols, t is torch.bfloat16)
-    ws = _workspace(n, dev)
+    ws = _workspace(n, src)
     rc = L.lc_orthogonalize(m, rows, cols, t is torch.bfloat16, _rows(where, "src", src, shape, t, dev),
                             _rows(where, "out", out, shape, t, dev), int(steps), ws.data_ptr(), n, stream.cuda_stream)
     if rc:
@@ -493,7 +499,7 @@ def update_orthogonal(X, V, G, lr: float, beta: float, wd: float = 0.0, steps: i
     m, rows, cols = shape
     L = lib()
     n = L.lc_orthogonal_workspace_bytes(m, rows, cols, GEMM_FP32)
-    ws = _workspace(n, dev)
+    ws = _workspace(n, X)
     rc = L.lc_update_orthogonal(m, rows, cols, *(_rows(where, k, t, shape, f32, dev) for t, k in ((X, "X"), (V, "V"), (G, "G"))),
                                 lr, beta, wd, int(steps), ws.data_ptr(), n, stream.cuda_stream)
     if rc:

@@ -81,7 +81,20 @@ __global__ void __launch_bounds__(1024) head_rows_kernel(const int32_t* labels, 
 
 // ------------------------------------------------------------------ operands
 
+// What the row kernel reads and writes, for batches whose gathering workgroups order the rows themselves (labels not null).
+struct RowArgs {
+    const int32_t* labels;
+    int64_t label_rep;
+    int rows, classes;
+    int32_t *order, *kept_label;
+    int* kept;
+    float* row_loss;
+    int64_t loss_rep;
+};
+constexpr int kOwnRows = kBlock;   // rows of such a batch at most: a thread each
+
 struct GatherArgs {
+    RowArgs own;
     const void* A;
     int64_t a_row, a_rep;
     const int32_t* order;
@@ -96,15 +109,44 @@ struct GatherArgs {
 template <typename T>
 __global__ void __launch_bounds__(kBlock) head_gather_kernel(GatherArgs g) {
     __shared__ float tile[64][65];
+    __shared__ int32_t own[kOwnRows];
+    __shared__ int part[kBlock / 64];
     const int i = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tc = threadIdx.x & 63, tr = threadIdx.x >> 6;
-    const int kept = g.kept[i] - g.base;
+    const int32_t* order = g.order + i * g.order_rep + g.base;
+    int kept;
+    if (g.own.labels) {
+        const RowArgs& o = g.own;
+        const int r = threadIdx.x, y = r < o.rows ? o.labels[i * o.label_rep + r] : -1;
+        const bool keep = y >= 0 && y < o.classes;
+        const uint64_t mask = __ballot(keep);
+        if (tc == 0) part[tr] = __popcll(mask);
+        __syncthreads();
+        int mine = __popcll(mask & ((1ULL << tc) - 1));
+        kept = 0;
+        for (int k = 0; k < kBlock / 64; ++k) {
+            if (k < tr) mine += part[k];
+            kept += part[k];
+        }
+        const int at = keep ? mine : kept + r - mine;
+        if (r < o.rows) own[at] = r;
+        if (blockIdx.x == 0 && blockIdx.y == 0 && r < o.rows) {   // for the kernels behind this one
+            o.order[(int64_t)i * o.rows + at] = r;
+            o.kept_label[(int64_t)i * o.rows + at] = keep ? y : -1;
+            if (!keep) o.row_loss[i * o.loss_rep + r] = 0.f;
+            if (r == 0) o.kept[i] = kept;
+        }
+        __syncthreads();
+        order = own;
+    } else {
+        kept = g.kept[i] - g.base;
+    }
     if (r0 >= kept) return;   // no product reads them
     const T* A = static_cast<const T*>(g.A) + i * g.a_rep;
     constexpr bool three = sizeof(T) == 4;
     int64_t row[16];
     float val[16];
 #pragma unroll
-    for (int q = 0; q < 16; ++q) row[q] = g.order[i * g.order_rep + g.base + min(r0 + q * 4 + tr, kept - 1)];
+    for (int q = 0; q < 16; ++q) row[q] = order[min(r0 + q * 4 + tr, kept - 1)];
 #pragma unroll
     for (int q = 0; q < 16; ++q) val[q] = static_cast<float>(A[row[q] * g.a_row + min(c0 + tc, g.d - 1)]);
 #pragma unroll
@@ -290,10 +332,9 @@ __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, Lo
 }
 
 // The parts of a row joined, a wavefront a row: its loss, the factor that makes dZ of each part's e, and the label's delta.
-__global__ void __launch_bounds__(kBlock) head_join_kernel(LogitArgs l, const int32_t* order, float e_unit, float* coef, float* delta_label,
-                                                           float* row_loss, int64_t loss_rep) {
-    const int i = blockIdx.y, lane = threadIdx.x & 63, m = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int kept = l.kept[i] - l.base;
+__device__ __forceinline__ void join_row(const LogitArgs& l, int i, int m, const int32_t* order, float e_unit, float* coef, float* delta_label,
+                                         float* row_loss, int64_t loss_rep) {
+    const int lane = threadIdx.x & 63, kept = l.kept[i] - l.base;
     if (m >= kept || m >= l.n) return;
     const int64_t at = (int64_t)i * l.n + m;
     const float2* st = l.stat + at * l.parts;
@@ -318,15 +359,39 @@ __global__ void __launch_bounds__(kBlock) head_join_kernel(LogitArgs l, const in
     }
 }
 
-__global__ void __launch_bounds__(kBlock) head_mean_kernel(const float* row_loss, int64_t loss_rep, int rows, const int* kept, float* loss) {
-    __shared__ double lds[4];
-    const int i = blockIdx.x;
+__global__ void __launch_bounds__(kBlock) head_join_kernel(LogitArgs l, const int32_t* order, float e_unit, float* coef, float* delta_label,
+                                                           float* row_loss, int64_t loss_rep) {
+    join_row(l, blockIdx.y, blockIdx.x * 4 + (threadIdx.x >> 6), order, e_unit, coef, delta_label, row_loss, loss_rep);
+}
+
+// The mean over a replica's rows, a workgroup's work.
+struct MeanArgs {
+    const float* row_loss;
+    int64_t loss_rep;
+    int rows;
+    const int* kept;
+    float* loss;                 // null: not here
+};
+__device__ __forceinline__ void mean_loss(const MeanArgs& a, int i) {
+    __shared__ double lds[16];
     double s = 0.0;
-    for (int r = threadIdx.x; r < rows; r += kBlock) s += row_loss[i * loss_rep + r];
+    for (int r = threadIdx.x; r < a.rows; r += blockDim.x) s += a.row_loss[i * a.loss_rep + r];
     s = wave_sum(s);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) loss[i] = kept[i] ? static_cast<float>(((lds[0] + lds[1]) + (lds[2] + lds[3])) / kept[i]) : 0.f;
+    if (threadIdx.x == 0) {
+        for (int k = 1; k < static_cast<int>(blockDim.x >> 6); ++k) s += lds[k];
+        a.loss[i] = a.kept[i] ? static_cast<float>(s / a.kept[i]) : 0.f;
+    }
+}
+__global__ void __launch_bounds__(kBlock) head_mean_kernel(MeanArgs a) { mean_loss(a, blockIdx.x); }
+
+// A replica's few rows joined and their mean, where nothing but the loss is asked for.
+constexpr int kFewRows = 16;   // a wavefront each
+__global__ void __launch_bounds__(64 * kFewRows) head_join_few_kernel(LogitArgs l, const int32_t* order, float* row_loss, MeanArgs a) {
+    join_row(l, blockIdx.x, threadIdx.x >> 6, order, 1.f, nullptr, nullptr, row_loss, a.loss_rep);
+    __syncthreads();   // the workgroup's own stores: visible to it behind the barrier
+    mean_loss(a, blockIdx.x);
 }
 
 // ------------------------------------------------------------------ dZ
@@ -449,9 +514,9 @@ struct FinishArgs {
     void* db;                    // or null
     int64_t db_rep;
 };
-// Grid: (rows, then 256 classes a workgroup; replicas).
+// Grid: (rows, then 256 classes a workgroup, then the mean; replicas).
 template <typename T, typename G>
-__global__ void __launch_bounds__(kBlock) head_finish_kernel(FinishArgs f, Across x) {
+__global__ void __launch_bounds__(kBlock) head_finish_kernel(FinishArgs f, Across x, MeanArgs mean) {
     const int i = blockIdx.y;
     const float unit = per_row(f.kept, i);
     if (static_cast<int>(blockIdx.x) < f.here) {
@@ -466,6 +531,10 @@ __global__ void __launch_bounds__(kBlock) head_finish_kernel(FinishArgs f, Acros
             }
             to[c] = static_cast<T>(s * unit);
         }
+        return;
+    }
+    if (mean.loss && blockIdx.x == gridDim.x - 1) {
+        mean_loss(mean, i);
         return;
     }
     const int c = (blockIdx.x - f.here) * kBlock + threadIdx.x;
@@ -684,7 +753,11 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
     const int rows = static_cast<int>(h.rows);
     float* row_loss = h.row_loss ? h.row_loss : p.row_loss;
     const int64_t loss_rep = h.row_loss ? h.row_loss_replica : rows;
-    head_rows_kernel<<<h.m, 1024, 0, st>>>(h.labels, h.label_replica, rows, h.classes, p.order, p.label, p.kept, row_loss, loss_rep);
+    const bool own = rows > 0 && rows <= kOwnRows;   // one chunk: its workgroups order the rows, a launch less
+    if (!own)
+        head_rows_kernel<<<h.m, 1024, 0, st>>>(h.labels, h.label_replica, rows, h.classes, p.order, p.label, p.kept, row_loss, loss_rep);
+    const MeanArgs mean{row_loss, loss_rep, rows, p.kept, h.loss};
+    const bool few = !p.grad && rows > 0 && rows <= kFewRows;
     const int64_t n = p.chunk;
     const T *A = static_cast<const T*>(h.A.p), *W = static_cast<const T*>(h.W.p);
     for (int g0 = 0; g0 < h.m; g0 += p.group) {
@@ -701,7 +774,11 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
         const int chunks = rows ? static_cast<int>((rows + n - 1) / n) : p.grad ? 1 : 0;   // no rows: gradients of zero
         for (int k = 0; k < chunks; ++k) {
             const int base = static_cast<int>(k * n), here = static_cast<int>(std::min<int64_t>(n, rows - base));
-            const GatherArgs ga{A + g0 * h.A.replica, h.A.row, h.A.replica, order, kept, rows, base, static_cast<int>(n), p.d, p.dp, p.a,
+            RowArgs rows_of{};
+            if (own)
+                rows_of = RowArgs{h.labels + g0 * h.label_replica, h.label_replica, rows, h.classes, p.order + (int64_t)g0 * rows,
+                                  p.label + (int64_t)g0 * rows, p.kept + g0, row_loss + g0 * loss_rep, loss_rep};
+            const GatherArgs ga{rows_of, A + g0 * h.A.replica, h.A.row, h.A.replica, order, kept, rows, base, static_cast<int>(n), p.d, p.dp, p.a,
                                 p.grad ? p.at : nullptr, a_part, at_part};
             if (here) head_gather_kernel<T><<<dim3(p.dp / 64, (here + 63) / 64, g), kBlock, 0, st>>>(ga);
             TileArgs t{};
@@ -730,7 +807,10 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
                 if (p.wide == 128 && rows <= 64) logits(typename Tiles<sizeof(T) == 4>::Few());
                 else if (p.wide == 128) logits(typename Tiles<sizeof(T) == 4>::Half());
                 else with_tile<sizeof(T) == 4>(t, logits);
-                head_join_kernel<<<dim3((here + 3) / 4, g), kBlock, 0, st>>>(l, order, p.three ? 1.f : 1.f / kEScale, p.coef,
+                if (few)
+                    head_join_few_kernel<<<g, 64 * kFewRows, 0, st>>>(l, order, row_loss + g0 * loss_rep,
+                                                                      MeanArgs{row_loss + g0 * loss_rep, loss_rep, rows, kept, h.loss + g0});
+                else head_join_kernel<<<dim3((here + 3) / 4, g), kBlock, 0, st>>>(l, order, p.three ? 1.f : 1.f / kEScale, p.coef,
                                                                             p.delta_label, row_loss + g0 * loss_rep, loss_rep);
             }
             if (!p.grad) continue;
@@ -766,8 +846,12 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             const FinishArgs fa{p.da, p.splits, static_cast<int>(n), p.d, p.d4, here, order, rows, kept, base, static_cast<T*>(h.dA.p) + g0 * h.dA.replica,
                                 h.dA.row, h.dA.replica, p.db_part, row_blocks, h.classes, p.ep,
                                 h.db ? static_cast<G*>(h.db) + g0 * h.db_replica : nullptr, h.db_replica};
-            const unsigned finish = here + (h.db ? (h.classes + kBlock - 1) / kBlock : 0);
-            if (finish) head_finish_kernel<T, G><<<dim3(finish, g), kBlock, 0, st>>>(fa, x);
+            MeanArgs last = mean;
+            last.row_loss += g0 * loss_rep;
+            last.kept += g0;
+            last.loss = x.last ? h.loss + g0 : nullptr;
+            const unsigned finish = here + (h.db ? (h.classes + kBlock - 1) / kBlock : 0) + (x.last ? 1 : 0);
+            if (finish) head_finish_kernel<T, G><<<dim3(finish, g), kBlock, 0, st>>>(fa, x, last);
             // dW = A^T dZ
             t = TileArgs{};
             t.a = TileOperand{p.at, n, p.d * n, {}, p.d, static_cast<int>(n)};
@@ -788,7 +872,7 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             });
         }
     }
-    head_mean_kernel<<<h.m, kBlock, 0, st>>>(row_loss, loss_rep, rows, p.kept, h.loss);
+    if (!p.grad && !few) head_mean_kernel<<<h.m, kBlock, 0, st>>>(mean);
     return hipGetLastError() == hipSuccess ? LC_OK : LC_ERR_HIP;
 }
 
