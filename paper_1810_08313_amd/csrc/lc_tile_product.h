@@ -11,8 +11,10 @@
 // A workgroup owns a BM x BN tile.  Tiles of BK k of both operands go from global memory straight into
 // LDS (16 bytes a lane, no registers), into two to four buffers in turn.  16-byte chunks are permuted inside a row,
 // by permuting what each lane fetches, so that the operand reads of a wavefront spread over all banks:
-//   KMajor  row of 64 k = 8 chunks:    chunk c of row r at c ^ ((r >> 1) & 7);  of 32 k: at c ^ ((r >> 2) & 3)
-//   NMajor  row of BN n, 32-byte pairs: pair p of row k at p ^ ((k & 3) | (k >> 3 & 1) << 2), as far as there are pairs
+//   KMajor  row of 64 k = 8 chunks:    chunk c of row r at c ^ ((r >> 1) & 7);  of 32 k: at c ^ (-(r >> 2) & 3)
+//   NMajor  row of BN n, 32-byte pairs: pair p of row k at p ^ ((k & 3) | (k >> 3 & 1) << 2);  of 64 n: at p ^ ((k >> 1 & 1) | (k >> 3 & 1) << 1)
+// (A 16-byte read serves lanes 0 to 3, 12 to 15 and 20 to 27 together: with c ^ ((r >> 2) & 3) for 32 k, every second
+// cycle was a conflict.)
 //
 // What bounds it: 64 KB of operands a k tile of 64 come out of the caches at about 10 TB/s over the chip (8192^3, where
 // 8 x 4 tiles of an XCD share them: 0.9 ms alone), LDS reads and the matrix cores could do 0.5 and 0.7 ms: 1.16 ms
@@ -84,6 +86,12 @@ struct TileShape {
     static_assert(BM * BK % (8 * kThreads) == 0 && kLds * 2 <= 160 * 1024 && TM % 2 == 0, "");
 };
 
+// What the place of a row's chunks (KMajor) or pairs (NMajor) is permuted with.
+template <int BK>
+__device__ __forceinline__ int k_place(int row) { return BK == 64 ? row >> 1 & 7 : -(row >> 2) & 3; }
+template <int BN>
+__device__ __forceinline__ int n_place(int k) { return BN == 64 ? (k >> 1 & 1) | (k >> 3 & 1) << 1 : (k & 3) | (k >> 3 & 1) << 2; }
+
 typedef __attribute__((address_space(3))) void* LdsPtr;
 typedef const __attribute__((address_space(1))) void* GlobalPtr;
 
@@ -102,7 +110,7 @@ struct KMajorFetch {
     __device__ __forceinline__ void init(const TileOperand& o, int row0) {
         const int t = threadIdx.x;
         static_assert(kPer % 16 == 0, "the permutation of a lane's chunk is the same in all its rows");
-        c8 = (BK == 64 ? (t & 7) ^ ((t >> 4) & 7) : (t & 3) ^ ((t >> 4) & 3)) * 8;
+        c8 = (t % kChunks ^ k_place<BK>(t / kChunks)) * 8;
 #pragma unroll
         for (int q = 0; q < kLoads; ++q)
             off[q] = ((uint32_t)(min(row0 + q * kPer + t / kChunks, o.rows - 1) - row0) * (uint32_t)o.row + c8) * 2u;
@@ -128,7 +136,6 @@ struct NMajorFetch {
     uint32_t col;   // bytes
     int k;
     uint32_t row2;  // bytes of a row
-    __device__ __forceinline__ static int swizzle(int k) { return (((k & 3) | ((k >> 3 & 1) << 2)) & (BN / 16 - 1)) << 1; }
     uint32_t off[kLoads];
     __device__ __forceinline__ void init(const TileOperand& o, int n0) {
         const int t = threadIdx.x;
@@ -136,7 +143,7 @@ struct NMajorFetch {
         row2 = (uint32_t)o.row * 2u;
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
-            const int kk = q * kPer + k, c = (t % kChunks) ^ swizzle(kk);
+            const int kk = q * kPer + k, c = (t % kChunks) ^ n_place<BN>(kk) << 1;
             off[q] = (uint32_t)kk * row2 + (uint32_t)min(n0 + c * 8, o.len - 8) * 2u;
         }
     }
@@ -161,7 +168,7 @@ struct NMajorFetch {
 
 template <int BK>
 __device__ __forceinline__ s16x8 read_kmajor(const uint16_t* tile, int row, int ks, int lane) {
-    const int c = BK == 64 ? (ks * 4 + (lane >> 4)) ^ ((lane >> 1) & 7) : (lane >> 4) ^ ((lane >> 2) & 3);
+    const int c = (ks * 4 + (lane >> 4)) ^ k_place<BK>(lane & 15);   // `row` is a multiple of 16
     return *reinterpret_cast<const s16x8*>(tile + (row + (lane & 15)) * BK + c * 8);
 }
 // A 16-lane group reads 4 rows of k, 16 columns; lane i gets column i of all four.
@@ -169,7 +176,7 @@ template <int BN>
 __device__ __forceinline__ s16x8 read_nmajor(const uint16_t* tile, int col, int ks, int lane) {
     const int g = lane >> 4, i = lane & 15;
     const int k = ks * 32 + g * 8 + (i >> 2);
-    const int pair = (col >> 4) ^ (((i >> 2) | ((g & 1) << 2)) & (BN / 16 - 1));
+    const int pair = (col >> 4) ^ n_place<BN>(k);   // the same for k + 4
     const uint16_t* at = tile + k * BN + pair * 16 + (i & 3) * 4;
     typedef __attribute__((address_space(3))) s16x4* P;
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)at);
@@ -197,10 +204,10 @@ struct AnyFetch {
             int row, x;
             if constexpr (NMAJOR) {
                 row = min(k0 + r, o.rows - 1);
-                x = x0 + (c ^ NMajorFetch<R, BK, THREADS>::swizzle(r)) * 8;
+                x = x0 + (c ^ n_place<R>(r) << 1) * 8;
             } else {
                 row = min(x0 + r, o.rows - 1) - x0;
-                x = k0 + (BK == 64 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3)) * 8;
+                x = k0 + (c ^ k_place<BK>(r)) * 8;
             }
             const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + (int64_t)row * o.row;
             if (x + 8 <= o.len) {
@@ -468,10 +475,8 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
 
 // A tile's sums through LDS, so that memory is reached in whole pieces of rows instead of 4 values a lane of 16 rows
 // (256 x 256, two parts each way: about 35 us a tile the one way, 20 the other).  The tile goes by slices of rows as LDS
-// holds them; 4-float groups of a row stand at n ^ sum_place(row), which spreads writes by 16 rows, reads along rows
-// and reads of 8 columns by 64 rows over all banks.
-__device__ __forceinline__ int sum_place(int row) { return (row & 15) << 2 ^ (row >> 4 & 3) << 3; }
-
+// holds them; 4-float groups of a row stand at n ^ place(row), which spreads writes by 16 rows, reads along rows
+// and reads of columns, 8 rows a lane, over all banks.
 template <typename S>
 struct SumSlices {
     static constexpr int fit() {
@@ -481,12 +486,13 @@ struct SumSlices {
     }
     static constexpr int kTiles = fit(), kRows = kTiles * 16 * S::WM, kCount = S::TM / kTiles;
     static_assert(kRows * S::BN * 4 <= S::kLds * 2 && S::BN % 64 == 0, "");
+    __device__ __forceinline__ static int place(int row) { return kRows >= 128 ? ((row & 15) ^ (row >> 4 & 7)) << 2 : (row & 15) << 2 ^ (row >> 4 & 3) << 3; }
     float* lds;
     __device__ __forceinline__ explicit SumSlices(uint16_t* l) : lds(reinterpret_cast<float*>(l)) {}
     // Row r of slice s is row row_of(s, r) of the tile.
     __device__ __forceinline__ static int row_of(int s, int r) { return (r / (kTiles * 16)) * S::TM * 16 + s * kTiles * 16 + r % (kTiles * 16); }
-    __device__ __forceinline__ float* at(int r, int n) const { return lds + r * S::BN + (n ^ sum_place(r)); }   // n % 4 == 0
-    __device__ __forceinline__ float& one(int r, int n) const { return lds[r * S::BN + (n ^ sum_place(r))]; }
+    __device__ __forceinline__ float* at(int r, int n) const { return lds + r * S::BN + (n ^ place(r)); }   // n % 4 == 0
+    __device__ __forceinline__ float& one(int r, int n) const { return lds[r * S::BN + (n ^ place(r))]; }
     template <int SL>
     __device__ __forceinline__ void put(const f32x4 (&acc)[S::TM][S::TN]) const {
         const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w / S::WN, wn = w % S::WN;
