@@ -166,7 +166,7 @@ __device__ __forceinline__ void store_factor(const Factors& f, int64_t at, float
 template <typename S, BLayout LB, OrthStep STEP>
 __global__ void __launch_bounds__(S::kThreads) orth_product_kernel(TileArgs a, OrthOut o) {
     __shared__ __align__(1024) uint16_t lds[S::kLds];
-    const TilePlace pl = tile_place<S>(a);
+    const TilePlace pl = tile_place<S>(a, blockIdx.x);
     if (pl.batch < 0) return;
     f32x4 acc[S::TM][S::TN];
     tile_sums<f16_t, S, LB>(a, pl, 0, a.K / S::BK, lds, acc);

@@ -107,11 +107,11 @@ struct GatherArgs {
 
 // 64 x 64 of the kept rows, as they are and transposed, zeros behind either end.
 template <typename T>
-__global__ void __launch_bounds__(kBlock) head_gather_kernel(GatherArgs g) {
+__device__ __forceinline__ void gather(const GatherArgs& g, int i, int block) {
     __shared__ float tile[64][65];
     __shared__ int32_t own[kOwnRows];
     __shared__ int part[kBlock / 64];
-    const int i = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tc = threadIdx.x & 63, tr = threadIdx.x >> 6;
+    const int across = g.dp / 64, r0 = block / across * 64, c0 = block % across * 64, tc = threadIdx.x & 63, tr = threadIdx.x >> 6;
     const int32_t* order = g.order + i * g.order_rep + g.base;
     int kept;
     if (g.own.labels) {
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kBlock) head_gather_kernel(GatherArgs g) {
         }
         const int at = keep ? mine : kept + r - mine;
         if (r < o.rows) own[at] = r;
-        if (blockIdx.x == 0 && blockIdx.y == 0 && r < o.rows) {   // for the kernels behind this one
+        if (block == 0 && r < o.rows) {   // for the kernels behind this one
             o.order[(int64_t)i * o.rows + at] = r;
             o.kept_label[(int64_t)i * o.rows + at] = keep ? y : -1;
             if (!keep) o.row_loss[i * o.loss_rep + r] = 0.f;
@@ -174,15 +174,24 @@ __global__ void __launch_bounds__(kBlock) head_gather_kernel(GatherArgs g) {
     }
 }
 
+constexpr int kCopyRows = 2048;   // most workgroups below each other
+
 // W as the products read it: rows of `cp` classes (a multiple of 8, zeros behind the last), fp32 in parts.
+struct WeightArgs {
+    const void* W;
+    int64_t row, rep;
+    int d, classes, cp, across, down;   // workgroups across a row, and rows at a time
+    uint16_t* out;
+    int64_t part;
+};
 template <typename T>
-__global__ void __launch_bounds__(kBlock) head_weights_kernel(const T* W, int64_t w_row, int64_t w_rep, int d, int classes, int cp,
-                                                              uint16_t* out, int64_t part) {
-    const int i = blockIdx.z;
-    for (int r = blockIdx.y; r < d; r += gridDim.y) {
-        const T* src = W + i * w_rep + r * w_row;
-        uint16_t* to = out + ((int64_t)i * d + r) * cp;
-        for (int c = (blockIdx.x * kBlock + threadIdx.x) * 8; c < cp; c += gridDim.x * kBlock * 8) {
+__device__ __forceinline__ void copy_weights(const WeightArgs& a, int i, int block) {
+    const int classes = a.classes, cp = a.cp;
+    const int64_t part = a.part;
+    for (int r = block / a.across; r < a.d; r += a.down) {
+        const T* src = static_cast<const T*>(a.W) + i * a.rep + r * a.row;
+        uint16_t* to = a.out + ((int64_t)i * a.d + r) * cp;
+        for (int c = (block % a.across * kBlock + threadIdx.x) * 8; c < cp; c += a.across * kBlock * 8) {
             T in[8];
             if (c + 8 <= classes) {
                 __builtin_memcpy(in, src + c, sizeof(in));
@@ -209,6 +218,14 @@ __global__ void __launch_bounds__(kBlock) head_weights_kernel(const T* W, int64_
     }
 }
 
+// Grid: the replicas' workgroups that gather (the longest: they also order), then those that copy weights.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) head_operands_kernel(GatherArgs g, int replicas, int gathering, WeightArgs w) {
+    const int i = static_cast<int>(blockIdx.x) % replicas, block = static_cast<int>(blockIdx.x) / replicas;
+    if (block < gathering) gather<T>(g, i, block);
+    else copy_weights<T>(w, i, block - gathering);
+}
+
 // ------------------------------------------------------------------ logits
 
 struct LogitArgs {
@@ -227,7 +244,7 @@ struct LogitArgs {
 template <typename S, typename E, BLayout LB>
 __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, LogitArgs l) {
     __shared__ __align__(1024) uint16_t lds[S::kLds];
-    const TilePlace pl = tile_place<S>(a);
+    const TilePlace pl = tile_place<S>(a, blockIdx.x);
     if (pl.batch < 0) return;
     const int kept = __builtin_amdgcn_readfirstlane(l.kept[pl.batch]) - l.base;
     if (pl.tm * S::BM >= kept) return;
@@ -332,10 +349,10 @@ __global__ void __launch_bounds__(S::kThreads) head_logits_kernel(TileArgs a, Lo
 }
 
 // The parts of a row joined, a wavefront a row: its loss, the factor that makes dZ of each part's e, and the label's delta.
+// coef: the row's, or null.
 __device__ __forceinline__ void join_row(const LogitArgs& l, int i, int m, const int32_t* order, float e_unit, float* coef, float* delta_label,
                                          float* row_loss, int64_t loss_rep) {
-    const int lane = threadIdx.x & 63, kept = l.kept[i] - l.base;
-    if (m >= kept || m >= l.n) return;
+    const int lane = threadIdx.x & 63;
     const int64_t at = (int64_t)i * l.n + m;
     const float2* st = l.stat + at * l.parts;
     const float zy = l.z_label[at];
@@ -349,19 +366,21 @@ __device__ __forceinline__ void join_row(const LogitArgs& l, int i, int m, const
     others = wave_sum(others);
     const float ey = expf(zy - ref), whole = others + ey, unit = 1.f / whole;
     if (coef)
-        for (int k = lane; k < l.parts; k += 64)
-            coef[at * l.parts + k] = expf((st[k].x == -INFINITY ? 0.f : st[k].x) - ref) * unit * e_unit;
+        for (int k = lane; k < l.parts; k += 64) coef[k] = expf((st[k].x == -INFINITY ? 0.f : st[k].x) - ref) * unit * e_unit;
     if (lane == 0) {
-        if (coef) delta_label[at] = -others * unit;
+        if (coef) *delta_label = -others * unit;
         // log(whole / ey); where the label's share is too small for that quotient, from the logits
         const float loss = others < 1e20f * ey ? log1pf(others / ey) : (ref + logf(whole)) - zy;
-        row_loss[i * loss_rep + order[(int64_t)i * l.label_rep + l.base + m]] = loss;
+        if (row_loss) row_loss[i * loss_rep + order[(int64_t)i * l.label_rep + l.base + m]] = loss;
     }
 }
 
 __global__ void __launch_bounds__(kBlock) head_join_kernel(LogitArgs l, const int32_t* order, float e_unit, float* coef, float* delta_label,
                                                            float* row_loss, int64_t loss_rep) {
-    join_row(l, blockIdx.y, blockIdx.x * 4 + (threadIdx.x >> 6), order, e_unit, coef, delta_label, row_loss, loss_rep);
+    const int i = blockIdx.y, m = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (m >= l.kept[i] - l.base || m >= l.n) return;
+    const int64_t at = (int64_t)i * l.n + m;
+    join_row(l, i, m, order, e_unit, coef ? coef + at * l.parts : nullptr, coef ? delta_label + at : nullptr, row_loss, loss_rep);
 }
 
 // The mean over a replica's rows, a workgroup's work.
@@ -389,7 +408,8 @@ __global__ void __launch_bounds__(kBlock) head_mean_kernel(MeanArgs a) { mean_lo
 // A replica's few rows joined and their mean, where nothing but the loss is asked for.
 constexpr int kFewRows = 16;   // a wavefront each
 __global__ void __launch_bounds__(64 * kFewRows) head_join_few_kernel(LogitArgs l, const int32_t* order, float* row_loss, MeanArgs a) {
-    join_row(l, blockIdx.x, threadIdx.x >> 6, order, 1.f, nullptr, nullptr, row_loss, a.loss_rep);
+    const int m = threadIdx.x >> 6;
+    if (m < l.kept[blockIdx.x]) join_row(l, blockIdx.x, m, order, 1.f, nullptr, nullptr, row_loss, a.loss_rep);
     __syncthreads();   // the workgroup's own stores: visible to it behind the barrier
     mean_loss(a, blockIdx.x);
 }
@@ -409,10 +429,27 @@ struct DeltaArgs {
 };
 
 // block_rows rows x 2048 classes a workgroup, 8 classes a thread, so that its columns' sums stay in registers.
-template <typename E>
-__global__ void __launch_bounds__(kBlock) head_delta_kernel(DeltaArgs d) {
+// JOIN: of few rows and parts, which it joins itself; every workgroup of a row does (8 x 64 rows, 1000 classes: 4.6 and 7.8 us
+// and a gap, 11.2 together).
+constexpr int kJoinRows = 16, kJoinParts = 64;
+struct JoinArgs {
+    LogitArgs l;
+    const int32_t* order;
+    float e_unit;
+    float* row_loss;
+    int64_t loss_rep;
+};
+template <typename E, bool JOIN>
+__global__ void __launch_bounds__(kBlock) head_delta_kernel(DeltaArgs d, JoinArgs j) {
+    __shared__ float coef[JOIN ? kJoinRows * kJoinParts : 1], delta[JOIN ? kJoinRows : 1];
     const int i = blockIdx.z, r0 = blockIdx.y * d.block_rows, c = (blockIdx.x * kBlock + threadIdx.x) * 8;
     const int kept = d.kept[i] - d.base;
+    if constexpr (JOIN) {
+        for (int r = threadIdx.x >> 6; r < d.block_rows; r += kBlock / 64)
+            if (r0 + r < kept)
+                join_row(j.l, i, r0 + r, j.order, j.e_unit, coef + r * kJoinParts, delta + r, blockIdx.x == 0 ? j.row_loss : nullptr, j.loss_rep);
+        __syncthreads();
+    }
     if (c >= d.ep) return;
     float sum[8];
 #pragma unroll
@@ -433,9 +470,9 @@ __global__ void __launch_bounds__(kBlock) head_delta_kernel(DeltaArgs d) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] = static_cast<float>(p[k]);
                 }
-                const float f = d.coef[((int64_t)i * d.n + r) * d.parts + c / d.wide];
+                const float f = JOIN ? coef[(r - r0) * kJoinParts + c / d.wide] : d.coef[((int64_t)i * d.n + r) * d.parts + c / d.wide];
                 const int y = d.label[i * d.label_rep + d.base + r] - c;
-                const float dy = d.delta_label[(int64_t)i * d.n + r];
+                const float dy = JOIN ? delta[r - r0] : d.delta_label[(int64_t)i * d.n + r];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     v[k] = k == y ? dy : v[k] * f;
@@ -477,9 +514,8 @@ __device__ __forceinline__ float per_row(const int* kept, int i) { return 1.f / 
 
 // Shares of dZ W^T over the classes, [splits][m][n][d] in 32 bits, d padded to 4.
 template <typename S, BLayout LB>
-__global__ void __launch_bounds__(S::kThreads) head_da_kernel(TileArgs a, float* out, int n_rows, int d) {
-    __shared__ __align__(1024) uint16_t lds[S::kLds];
-    const TilePlace pl = tile_place<S>(a);
+__device__ __forceinline__ void da_tile(const TileArgs& a, float* out, int n_rows, int d, uint16_t* lds, unsigned block) {
+    const TilePlace pl = tile_place<S>(a, block);
     if (pl.batch < 0) return;
     int k0, k1;
     tile_k_range<S>(a, pl, k0, k1);
@@ -496,6 +532,12 @@ __global__ void __launch_bounds__(S::kThreads) head_da_kernel(TileArgs a, float*
             const int m = mw + i * 16, n = nw + j * 16;
             if (m < a.M && n < d) *reinterpret_cast<f32x4*>(out + (int64_t)m * d + n) = acc[i][j];
         }
+}
+
+template <typename S, BLayout LB>
+__global__ void __launch_bounds__(S::kThreads) head_da_kernel(TileArgs a, float* out, int n_rows, int d) {
+    __shared__ __align__(1024) uint16_t lds[S::kLds];
+    da_tile<S, LB>(a, out, n_rows, d, lds, blockIdx.x);
 }
 
 // What is left of a chunk: dA's shares added up, each row to its place (rows that do not count get zeros), and db.
@@ -557,10 +599,18 @@ __device__ __forceinline__ void store8(bf16_t* to, const float (&v)[8]) {
     __builtin_memcpy(to, &h, 16);
 }
 
+template <typename G>
+struct DwOut {
+    Across x;
+    G* dW;
+    int64_t row, rep;
+};
 template <typename S, typename G>
-__global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across x, G* dW, int64_t row, int64_t rep) {
-    __shared__ __align__(1024) uint16_t lds[S::kLds];
-    const TilePlace pl = tile_place<S>(a);
+__device__ __forceinline__ void dw_tile(const TileArgs& a, const DwOut<G>& o, uint16_t* lds, unsigned block) {
+    const Across& x = o.x;
+    G* dW = o.dW;
+    const int64_t row = o.row, rep = o.rep;
+    const TilePlace pl = tile_place<S>(a, block);
     if (pl.batch < 0) return;
     int k0, k1;
     tile_k_range<S>(a, pl, k0, k1);
@@ -599,6 +649,19 @@ __global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, Across
     });
 }
 
+template <typename S, typename G>
+__global__ void __launch_bounds__(S::kThreads) head_dw_kernel(TileArgs a, DwOut<G> o) {
+    __shared__ __align__(1024) uint16_t lds[S::kLds];
+    dw_tile<S, G>(a, o, lds, blockIdx.x);
+}
+// Both gradient products of a small problem, which neither fills the chip nor needs the other.
+template <typename S, BLayout LB, typename G>
+__global__ void __launch_bounds__(S::kThreads) head_grads_kernel(TileArgs a, float* out, int n_rows, int d, unsigned da_blocks, TileArgs b, DwOut<G> o) {
+    __shared__ __align__(1024) uint16_t lds[S::kLds];
+    if (blockIdx.x < da_blocks) da_tile<S, LB>(a, out, n_rows, d, lds, blockIdx.x);
+    else dw_tile<S, G>(b, o, lds, blockIdx.x - da_blocks);
+}
+
 // ------------------------------------------------------------------ host
 
 // Tiles of the products: one part (bf16 operands) or three (fp32).
@@ -618,6 +681,10 @@ struct Tiles<true> {
     typedef TileShape<128, 256, 2, 4, 32, 3, 2> Rows128;
     typedef Rows128 Rows256;   // 256 x 256 in three parts would take 192 KB of LDS for two buffers
 };
+
+// Workgroups of both gradient products together up to which they are one launch of the smallest tiles: neither fills the
+// chip (8 x 64 rows, 256 x 1000, fp32: 12.4 and 12.7 us and a gap, 13.6 together).
+constexpr unsigned kBothGrads = 512;
 
 // A product's tile by its rows: no taller than they need, 256 where there are more.
 template <bool THREE, typename F>
@@ -639,6 +706,8 @@ int head_wide(const lc_head_args& h) {
     if (h.rows > 128) return 256;
     return h.rows > 64 || (int64_t)h.m * ((h.classes + 255) / 256) < 256 ? 128 : 256;
 }
+
+int copy_across(int cp) { return std::min((cp + kBlock * 8 - 1) / (kBlock * 8), 64); }
 
 struct HeadPlan {
     bool grad, three, copy_w, any_w;   // gradients; fp32 operands in three parts; W copied first, or of any alignment
@@ -701,6 +770,9 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
     const int64_t few = std::min<int64_t>(rows, 256);
     p.group = static_cast<int>(std::min<int64_t>(h.m, std::max<int64_t>(1, kKeepBytes / (per_row * few))));
     p.chunk = static_cast<int>(std::min<int64_t>({rows, 65536, std::max<int64_t>(few, kKeepBytes / (per_row * p.group) / 256 * 256)}));
+    // a launch has below 2^32 threads: head_operands_kernel's workgroups
+    const int64_t blocks = p.dp / 64 * (p.chunk / 64) + (p.copy_w ? copy_across(p.cp) * std::min(p.d, kCopyRows) : 0);
+    p.group = static_cast<int>(std::min<int64_t>(p.group, std::max<int64_t>(1, (int64_t{1} << 23) / blocks)));
     const int np = p.three ? 3 : 1;
     const int64_t g = p.group, n = p.chunk;
     Carver c{static_cast<char*>(ws)};
@@ -758,6 +830,7 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
         head_rows_kernel<<<h.m, 1024, 0, st>>>(h.labels, h.label_replica, rows, h.classes, p.order, p.label, p.kept, row_loss, loss_rep);
     const MeanArgs mean{row_loss, loss_rep, rows, p.kept, h.loss};
     const bool few = !p.grad && rows > 0 && rows <= kFewRows;
+    const bool join_there = p.grad && p.block_rows <= kJoinRows && p.parts <= kJoinParts;
     const int64_t n = p.chunk;
     const T *A = static_cast<const T*>(h.A.p), *W = static_cast<const T*>(h.W.p);
     for (int g0 = 0; g0 < h.m; g0 += p.group) {
@@ -766,9 +839,10 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
         const int32_t *order = p.order + (int64_t)g0 * rows, *label = p.label + (int64_t)g0 * rows;
         const int* kept = p.kept + g0;
         TileOperand w{reinterpret_cast<const uint16_t*>(W + g0 * h.W.replica), h.W.row, h.W.replica, {}, p.d, h.classes};
+        WeightArgs wa{};
         if (p.copy_w) {
-            const dim3 grid(static_cast<unsigned>(std::min((p.cp + kBlock * 8 - 1) / (kBlock * 8), 64)), std::min(p.d, 2048), g);
-            head_weights_kernel<T><<<grid, kBlock, 0, st>>>(W + g0 * h.W.replica, h.W.row, h.W.replica, p.d, h.classes, p.cp, p.w, w_part);
+            wa = WeightArgs{W + g0 * h.W.replica, h.W.row, h.W.replica, p.d, h.classes, p.cp, copy_across(p.cp),
+                            std::min(p.d, kCopyRows), p.w, w_part};
             w = TileOperand{p.w, p.cp, (int64_t)p.d * p.cp, {}, p.d, p.cp};
         }
         const int chunks = rows ? static_cast<int>((rows + n - 1) / n) : p.grad ? 1 : 0;   // no rows: gradients of zero
@@ -780,7 +854,10 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
                                   p.label + (int64_t)g0 * rows, p.kept + g0, row_loss + g0 * loss_rep, loss_rep};
             const GatherArgs ga{rows_of, A + g0 * h.A.replica, h.A.row, h.A.replica, order, kept, rows, base, static_cast<int>(n), p.d, p.dp, p.a,
                                 p.grad ? p.at : nullptr, a_part, at_part};
-            if (here) head_gather_kernel<T><<<dim3(p.dp / 64, (here + 63) / 64, g), kBlock, 0, st>>>(ga);
+            if (here) {
+                const int gathering = p.dp / 64 * ((here + 63) / 64), copying = k == 0 ? wa.across * wa.down : 0;
+                head_operands_kernel<T><<<static_cast<unsigned>(g * (gathering + copying)), kBlock, 0, st>>>(ga, g, gathering, wa);
+            }
             TileArgs t{};
             t.a = TileOperand{p.a, p.dp, n * p.dp, {}, here, p.dp};
             t.b = w;
@@ -810,14 +887,19 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
                 if (few)
                     head_join_few_kernel<<<g, 64 * kFewRows, 0, st>>>(l, order, row_loss + g0 * loss_rep,
                                                                       MeanArgs{row_loss + g0 * loss_rep, loss_rep, rows, kept, h.loss + g0});
-                else head_join_kernel<<<dim3((here + 3) / 4, g), kBlock, 0, st>>>(l, order, p.three ? 1.f : 1.f / kEScale, p.coef,
+                else if (!join_there) head_join_kernel<<<dim3((here + 3) / 4, g), kBlock, 0, st>>>(l, order, p.three ? 1.f : 1.f / kEScale, p.coef,
                                                                             p.delta_label, row_loss + g0 * loss_rep, loss_rep);
             }
             if (!p.grad) continue;
             const int row_blocks = static_cast<int>(round_up(here, 64)) / p.block_rows;
             const DeltaArgs da{l.e, p.dz, p.ep, dz_part, p.coef, p.delta_label, label, kept, rows, base, static_cast<int>(n), p.parts, p.wide,
                                h.classes, row_blocks, p.block_rows, p.db_part};
-            if (here) head_delta_kernel<E><<<dim3(static_cast<unsigned>((p.ep + kBlock * 8 - 1) / (kBlock * 8)), row_blocks, g), kBlock, 0, st>>>(da);
+            if (here) {
+                const dim3 grid(static_cast<unsigned>((p.ep + kBlock * 8 - 1) / (kBlock * 8)), row_blocks, g);
+                const JoinArgs ja{l, order, p.three ? 1.f : 1.f / kEScale, row_loss + g0 * loss_rep, loss_rep};
+                if (join_there) head_delta_kernel<E, true><<<grid, kBlock, 0, st>>>(da, ja);
+                else head_delta_kernel<E, false><<<grid, kBlock, 0, st>>>(da, ja);
+            }
             Across x{k == 0, k + 1 == chunks, p.db_acc, kept};
             // dA = dZ W^T
             t = TileArgs{};
@@ -831,16 +913,45 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             t.splits = p.splits;
             t.m_count = kept;
             t.count_base = base;
-            if (here) {
-                with_tile<sizeof(T) == 4>(t, [&](auto s) {
-                    typedef decltype(s) S;
-                    if constexpr (sizeof(T) == 2) {
-                        if (p.any_w) {
-                            head_da_kernel<S, KMajorAny><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, p.da, static_cast<int>(n), p.d4);
-                            return;
+            // dW = A^T dZ
+            TileArgs u{};
+            u.a = TileOperand{p.at, n, p.d * n, {}, p.d, static_cast<int>(n)};
+            u.b = TileOperand{p.dz, p.ep, n * p.ep, {}, static_cast<int>(n), static_cast<int>(p.ep)};
+            set_parts(u, at_part, dz_part);
+            u.M = p.d;
+            u.N = h.classes;
+            u.K = static_cast<int>(round_up(here, kPadK));
+            u.batches = g;
+            u.splits = 1;
+            u.k_count = kept;
+            u.count_base = base;
+            const DwOut<G> dw{{x.first, x.last, p.dw_acc, kept}, static_cast<G*>(h.dW.p) + g0 * h.dW.replica, h.dW.row, h.dW.replica};
+            typedef typename Tiles<sizeof(T) == 4>::Rows64 Small;
+            const unsigned da_blocks = tile_grid<Small>(t), dw_blocks = tile_grid<Small>(u);
+            const int n_rows = static_cast<int>(n);
+            if (here && da_blocks + dw_blocks <= kBothGrads) {
+                const unsigned grid = da_blocks + dw_blocks;
+                if constexpr (sizeof(T) == 2) {
+                    if (p.any_w) head_grads_kernel<Small, KMajorAny, G><<<grid, Small::kThreads, 0, st>>>(t, p.da, n_rows, p.d4, da_blocks, u, dw);
+                    else head_grads_kernel<Small, KMajor, G><<<grid, Small::kThreads, 0, st>>>(t, p.da, n_rows, p.d4, da_blocks, u, dw);
+                } else {
+                    head_grads_kernel<Small, KMajor, G><<<grid, Small::kThreads, 0, st>>>(t, p.da, n_rows, p.d4, da_blocks, u, dw);
+                }
+            } else {
+                if (here)
+                    with_tile<sizeof(T) == 4>(t, [&](auto s) {
+                        typedef decltype(s) S;
+                        if constexpr (sizeof(T) == 2) {
+                            if (p.any_w) {
+                                head_da_kernel<S, KMajorAny><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, p.da, n_rows, p.d4);
+                                return;
+                            }
                         }
-                    }
-                    head_da_kernel<S, KMajor><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, p.da, static_cast<int>(n), p.d4);
+                        head_da_kernel<S, KMajor><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, p.da, n_rows, p.d4);
+                    });
+                with_tile<sizeof(T) == 4>(u, [&](auto s) {
+                    typedef decltype(s) S;
+                    head_dw_kernel<S, G><<<tile_grid<S>(u), S::kThreads, 0, st>>>(u, dw);
                 });
             }
             const FinishArgs fa{p.da, p.splits, static_cast<int>(n), p.d, p.d4, here, order, rows, kept, base, static_cast<T*>(h.dA.p) + g0 * h.dA.replica,
@@ -852,24 +963,6 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             last.loss = x.last ? h.loss + g0 : nullptr;
             const unsigned finish = here + (h.db ? (h.classes + kBlock - 1) / kBlock : 0) + (x.last ? 1 : 0);
             if (finish) head_finish_kernel<T, G><<<dim3(finish, g), kBlock, 0, st>>>(fa, x, last);
-            // dW = A^T dZ
-            t = TileArgs{};
-            t.a = TileOperand{p.at, n, p.d * n, {}, p.d, static_cast<int>(n)};
-            t.b = TileOperand{p.dz, p.ep, n * p.ep, {}, static_cast<int>(n), static_cast<int>(p.ep)};
-            set_parts(t, at_part, dz_part);
-            t.M = p.d;
-            t.N = h.classes;
-            t.K = static_cast<int>(round_up(here, kPadK));
-            t.batches = g;
-            t.splits = 1;
-            t.k_count = kept;
-            t.count_base = base;
-            x.acc = p.dw_acc;
-            G* dW = static_cast<G*>(h.dW.p) + g0 * h.dW.replica;
-            with_tile<sizeof(T) == 4>(t, [&](auto s) {
-                typedef decltype(s) S;
-                head_dw_kernel<S, G><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, x, dW, h.dW.row, h.dW.replica);
-            });
         }
     }
     if (!p.grad && !few) head_mean_kernel<<<h.m, kBlock, 0, st>>>(mean);

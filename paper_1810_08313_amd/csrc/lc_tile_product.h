@@ -268,12 +268,12 @@ __device__ __forceinline__ bool mirrored(int m, int n) { return n / S::BM * S::B
 // Workgroup id -> tile.  Each XCD takes a contiguous range; inside it, blocks of 8 tiles of M by all of N, M fastest,
 // so that what runs together shares rows of A and columns of B in the L2.
 template <typename S>
-__device__ __forceinline__ TilePlace tile_place(const TileArgs& a) {
+__device__ __forceinline__ TilePlace tile_place(const TileArgs& a, unsigned block) {
     const int64_t total = (int64_t)a.per_batch * a.batches * a.splits;
     const int64_t chunk = (total + kXcds - 1) / kXcds;
-    const int64_t id = (int64_t)(blockIdx.x % kXcds) * chunk + blockIdx.x / kXcds;
+    const int64_t id = (int64_t)(block % kXcds) * chunk + block / kXcds;
     TilePlace pl{-1, 0, 0, 0};
-    if (blockIdx.x / kXcds >= chunk || id >= total) return pl;
+    if (block / kXcds >= chunk || id >= total) return pl;
     const int64_t one = id % ((int64_t)a.per_batch * a.splits);
     pl.batch = (int)(id / ((int64_t)a.per_batch * a.splits));
     pl.split = (int)(one / a.per_batch);

@@ -332,3 +332,18 @@ def test_bindings_refuse(pkg):
     for f in bad:
         with pytest.raises(pkg.LcError):
             f()
+
+
+def test_more_replicas_than_a_launch_has_threads_for(pkg):
+    import torch
+    m, d, classes = 65535, 1030, 3
+    A, W, b, y = _inputs(m, 1, d, classes, False, 41)
+    loss, dA, dW, db = pkg.softmax_head_grad(A, W, b, y)
+    for i in (0, 1, 4095, 8011, 8012, 40000, m - 1):
+        want = _reference(A[i], W[i], b[i], y[i])
+        _check("loss", loss[i], want["loss"], want["loss_tol"])
+        _check("dA", dA[i], want["dA"], want["dA_tol"])
+        _check("dW", dW[i], want["dW"], want["dW_tol"])
+        _check("db", db[i], want["db"], want["db_tol"])
+    ref = torch.nn.functional.cross_entropy((A[:, 0, :, None] * W).sum(1) + b, y[:, 0].long(), reduction="none")
+    assert torch.allclose(loss, ref, rtol=1e-3, atol=1e-3)
