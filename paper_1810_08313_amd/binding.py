@@ -283,8 +283,8 @@ def _refuse(where: str, what: str) -> None:
 
 
 def _first(where: str, t, stream):
-    """The stream of a call, from its first tensor [m, rows, cols], and whether it is not what torch's allocator would
-    take by itself."""
+    """A call's raw stream, from its first tensor [m, rows, cols], and the stream itself if torch's allocator would not
+    take it by itself (for _on), or None."""
     import torch
     if not t.is_cuda:
         _refuse(where, "tensors of a GPU are needed")
@@ -292,12 +292,14 @@ def _first(where: str, t, stream):
         _refuse(where, f"a tensor of shape {tuple(t.shape)} where [m, rows, cols] is needed")
     if t.dtype is not torch.float32 and t.dtype is not torch.bfloat16:
         _refuse(where, f"element type {t.dtype}")
-    here = torch.cuda.current_device() == t.get_device()
+    dev = t.get_device()
+    here = torch.cuda.current_device() == dev
+    raw = torch._C._cuda_getCurrentRawStream(dev)   # 0.2 us; a torch.cuda.Stream and its handle: 1.8
     if stream is None:
-        return torch.cuda.current_stream(t.device), not here
+        return raw, None if here else torch.cuda.current_stream(t.device)
     if stream.device != t.device:
         _refuse(where, "the stream is another device's")
-    return stream, not here or stream != torch.cuda.current_stream(t.device)
+    return stream.cuda_stream, None if here and stream.cuda_stream == raw else stream
 
 
 def _on(stream, *tensors):
@@ -352,9 +354,9 @@ def layer_norm(x, gain=None, bias=None, eps: float = 1e-5, out=None, stream=None
     Returns y and the statistics [m, rows, 2] that layer_norm_grad takes."""
     import torch
     where = "lc_layer_norm"
-    stream, other = _first(where, x, stream)
-    if other:
-        with _on(stream, x, gain, bias, out):
+    raw, other = _first(where, x, stream)
+    if other is not None:
+        with _on(other, x, gain, bias, out):
             return layer_norm(x, gain, bias, eps, out)
     f32, t, dev, shape = torch.float32, x.dtype, x.device, x.shape
     m, rows, cols = shape
@@ -365,7 +367,7 @@ def layer_norm(x, gain=None, bias=None, eps: float = 1e-5, out=None, stream=None
     if gs != bs and gp and bp and m > 1:
         _refuse(where, "gain and bias have different distances between replicas")
     rc = lib().lc_layer_norm(m, rows, cols, t is torch.bfloat16, _rows(where, "x", x, shape, t, dev), gp, bp, gs or bs, eps,
-                             _rows(where, "out", y, shape, t, dev), stats.data_ptr(), stream.cuda_stream)
+                             _rows(where, "out", y, shape, t, dev), stats.data_ptr(), raw)
     if rc:
         raise LcError(rc, where)
     return y, stats
@@ -375,9 +377,9 @@ def layer_norm_grad(x, dy, gain, stats, dx=None, dgain=None, dbias=None, stream=
     """lc_layer_norm_grad: dx, dgain and dbias (fp32 [m, cols]) from dy and what layer_norm returned."""
     import torch
     where = "lc_layer_norm_grad"
-    stream, other = _first(where, x, stream)
-    if other:
-        with _on(stream, x, dy, gain, stats, dx, dgain, dbias):
+    raw, other = _first(where, x, stream)
+    if other is not None:
+        with _on(other, x, dy, gain, stats, dx, dgain, dbias):
             return layer_norm_grad(x, dy, gain, stats, dx, dgain, dbias)
     f32, t, dev, shape = torch.float32, x.dtype, x.device, x.shape
     m, rows, cols = shape
@@ -401,13 +403,13 @@ def layer_norm_grad(x, dy, gain, stats, dx=None, dgain=None, dbias=None, stream=
     ws = _workspace(n, x)
     rc = L.lc_layer_norm_grad(m, rows, cols, t is torch.bfloat16, _rows(where, "x", x, shape, t, dev), _rows(where, "dy", dy, shape, t, dev),
                               gp, gs, stats.data_ptr(), _rows(where, "dx", dx, shape, t, dev), dgp, dbp, dgs, ws.data_ptr(), n,
-                              stream.cuda_stream)
+                              raw)
     if rc:
         raise LcError(rc, where)
     return dx, dgain, dbias
 
 
-def _softmax_head(where, A, W, bias, labels, stream, grads):
+def _softmax_head(where, A, W, bias, labels, raw, grads):
     import torch
     f32, t, dev = torch.float32, A.dtype, A.device
     m, rows, d = A.shape
@@ -439,7 +441,7 @@ def _softmax_head(where, A, W, bias, labels, stream, grads):
         out, fn = (loss, dA, dW, db), L.lc_softmax_head_grad
     n = L.lc_softmax_head_workspace_bytes(C.byref(h), grads is not None)
     ws = _workspace(n, A)
-    rc = fn(C.byref(h), ws.data_ptr(), n, stream.cuda_stream)
+    rc = fn(C.byref(h), ws.data_ptr(), n, raw)
     if rc:
         raise LcError(rc, where)
     return out
@@ -449,30 +451,30 @@ def softmax_head_loss(A, W, bias, labels, stream=None):
     """lc_softmax_head_loss: mean cross-entropy [m] of Z = A W + bias and the rows' [m, rows]; A [m, rows, inputs] and
     W [m, inputs, classes] fp32 or bfloat16, bias fp32 [m, classes] or None, labels int32 [m, rows]."""
     where = "lc_softmax_head_loss"
-    stream, other = _first(where, A, stream)
-    if other:
-        with _on(stream, A, W, bias, labels):
-            return _softmax_head(where, A, W, bias, labels, stream, None)
-    return _softmax_head(where, A, W, bias, labels, stream, None)
+    raw, other = _first(where, A, stream)
+    if other is not None:
+        with _on(other, A, W, bias, labels):
+            return _softmax_head(where, A, W, bias, labels, raw, None)
+    return _softmax_head(where, A, W, bias, labels, raw, None)
 
 
 def softmax_head_grad(A, W, bias, labels, dA=None, dW=None, db=None, grad_dtype=None, stream=None):
     """lc_softmax_head_grad: the loss [m], dA, dW and db (the last two of grad_dtype, A's element type by default)."""
     where = "lc_softmax_head_grad"
-    stream, other = _first(where, A, stream)
-    if other:
-        with _on(stream, A, W, bias, labels, dA, dW, db):
-            return _softmax_head(where, A, W, bias, labels, stream, (dA, dW, db, grad_dtype))
-    return _softmax_head(where, A, W, bias, labels, stream, (dA, dW, db, grad_dtype))
+    raw, other = _first(where, A, stream)
+    if other is not None:
+        with _on(other, A, W, bias, labels, dA, dW, db):
+            return _softmax_head(where, A, W, bias, labels, raw, (dA, dW, db, grad_dtype))
+    return _softmax_head(where, A, W, bias, labels, raw, (dA, dW, db, grad_dtype))
 
 
 def orthogonalize(src, steps: int = 5, out=None, stream=None):
     """lc_orthogonalize of src [m, rows, cols], fp32 or bfloat16."""
     import torch
     where = "lc_orthogonalize"
-    stream, other = _first(where, src, stream)
-    if other:
-        with _on(stream, src, out):
+    raw, other = _first(where, src, stream)
+    if other is not None:
+        with _on(other, src, out):
             return orthogonalize(src, steps, out)
     t, dev, shape = src.dtype, src.device, src.shape
     m, rows, cols = shape
@@ -481,7 +483,7 @@ def orthogonalize(src, steps: int = 5, out=None, stream=None):
     n = L.lc_orthogonal_workspace_bytes(m, rows, cols, t is torch.bfloat16)
     ws = _workspace(n, src)
     rc = L.lc_orthogonalize(m, rows, cols, t is torch.bfloat16, _rows(where, "src", src, shape, t, dev),
-                            _rows(where, "out", out, shape, t, dev), int(steps), ws.data_ptr(), n, stream.cuda_stream)
+                            _rows(where, "out", out, shape, t, dev), int(steps), ws.data_ptr(), n, raw)
     if rc:
         raise LcError(rc, where)
     return out
@@ -491,9 +493,9 @@ def update_orthogonal(X, V, G, lr: float, beta: float, wd: float = 0.0, steps: i
     """lc_update_orthogonal of X and V in place, fp32 [m, rows, cols] each."""
     import torch
     where = "lc_update_orthogonal"
-    stream, other = _first(where, X, stream)
-    if other:
-        with _on(stream, X, V, G):
+    raw, other = _first(where, X, stream)
+    if other is not None:
+        with _on(other, X, V, G):
             return update_orthogonal(X, V, G, lr, beta, wd, steps)
     f32, dev, shape = torch.float32, X.device, X.shape
     m, rows, cols = shape
@@ -501,7 +503,7 @@ def update_orthogonal(X, V, G, lr: float, beta: float, wd: float = 0.0, steps: i
     n = L.lc_orthogonal_workspace_bytes(m, rows, cols, GEMM_FP32)
     ws = _workspace(n, X)
     rc = L.lc_update_orthogonal(m, rows, cols, *(_rows(where, k, t, shape, f32, dev) for t, k in ((X, "X"), (V, "V"), (G, "G"))),
-                                lr, beta, wd, int(steps), ws.data_ptr(), n, stream.cuda_stream)
+                                lr, beta, wd, int(steps), ws.data_ptr(), n, raw)
     if rc:
         raise LcError(rc, where)
 
