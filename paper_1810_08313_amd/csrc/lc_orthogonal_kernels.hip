@@ -90,56 +90,6 @@ __device__ __forceinline__ void split(float x, uint16_t& h, uint16_t& l) {
     l = __builtin_bit_cast(uint16_t, static_cast<f16_t>(x - static_cast<float>(a)));
 }
 
-// M / |M| into X's parts, 64 x 64 a workgroup, transposed where M is higher than wide.
-template <typename T>
-__global__ void __launch_bounds__(kBlock) orth_start_kernel(OrthIn in, int n_parts, int tall, Factors f, int S, int Lp) {
-    __shared__ float tile[64][65];
-    __shared__ float inv_s;
-    const int i = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;   // of X
-    const T* src = static_cast<const T*>(in.src) + i * in.rep;
-    const float* v = in.v ? in.v + i * in.v_rep : nullptr;
-    if (threadIdx.x < 64) {
-        double part = 0.0;
-        for (int k = threadIdx.x; k < n_parts; k += 64) part += in.parts[i * kNormParts + k];
-        const double s = wave_sum(part);
-        // a zero matrix stays zero; a norm below what 1 / norm can be in 32 bits: as far as that goes
-        if (threadIdx.x == 0) inv_s = s > 0.0 ? static_cast<float>(fmin(1.0 / sqrt(s), 3e38)) : s == 0.0 ? 0.f : static_cast<float>(s);
-    }
-    __syncthreads();
-    const float inv = inv_s;
-    const int tc = threadIdx.x & 63, tr = threadIdx.x >> 6;
-#pragma unroll 4
-    for (int q = 0; q < 16; ++q) {
-        const int a = q * 4 + tr;   // row of the tile of M as it stands
-        const int r = (tall ? c0 : r0) + a, c = (tall ? r0 : c0) + tc;
-        float val = 0.f;
-        if (r < in.rows && c < in.cols) val = v ? v[r * in.v_row + c] : static_cast<float>(src[r * in.row + c]);
-        tile[a][tc] = val * inv;
-    }
-    __syncthreads();
-#pragma unroll 4
-    for (int q = 0; q < 16; ++q) {
-        const int r = r0 + q * 4 + tr, c = c0 + tc;
-        if (r >= S) continue;
-        const float val = tall ? tile[tc][q * 4 + tr] : tile[q * 4 + tr][tc];
-        const int64_t at = ((int64_t)i * S + r) * Lp + c;
-        uint16_t h, l;
-        split(val * kUp, h, l);
-        f.h[at] = h;
-        f.l[at] = l;
-    }
-}
-
-struct OrthOut {
-    int S, Sp, L, Lp;
-    Factors from, to;           // A or X that the step adds; A, B or the next X
-    // last step
-    int tall, update, out_bf16;
-    void* out;                  // M's place of the result, or X of the update
-    int64_t out_row, out_rep;
-    float lr, scale, wd;
-};
-
 struct Eight {
     f16x8 h, l;
     __device__ __forceinline__ void load(const Factors& f, int64_t at) {
@@ -162,6 +112,54 @@ __device__ __forceinline__ void store_factor(const Factors& f, int64_t at, float
     *reinterpret_cast<s16x8*>(f.h + at) = h;
     *reinterpret_cast<s16x8*>(f.l + at) = l;
 }
+
+// M / |M| into X's parts, 64 x 64 a workgroup, transposed where M is higher than wide.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) orth_start_kernel(OrthIn in, int n_parts, int tall, Factors f, int S, int Lp) {
+    __shared__ float tile[64][65];
+    __shared__ float inv_s;
+    const int i = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;   // of X
+    const T* src = static_cast<const T*>(in.src) + i * in.rep;
+    const float* v = in.v ? in.v + i * in.v_rep : nullptr;
+    const int tc = threadIdx.x & 63, tr = threadIdx.x >> 6;
+    float val[16];
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {   // rows of the tile of M as it stands
+        const int r = (tall ? c0 : r0) + q * 4 + tr, c = (tall ? r0 : c0) + tc;
+        val[q] = r < in.rows && c < in.cols ? v ? v[r * in.v_row + c] : static_cast<float>(src[r * in.row + c]) : 0.f;
+    }
+    if (threadIdx.x < 64) {
+        double part = 0.0;
+        for (int k = threadIdx.x; k < n_parts; k += 64) part += in.parts[i * kNormParts + k];
+        const double s = wave_sum(part);
+        // a zero matrix stays zero; a norm below what 1 / norm can be in 32 bits: as far as that goes
+        if (threadIdx.x == 0) inv_s = s > 0.0 ? static_cast<float>(fmin(1.0 / sqrt(s), 3e38)) : s == 0.0 ? 0.f : static_cast<float>(s);
+    }
+    __syncthreads();
+    const float inv = inv_s;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) tile[q * 4 + tr][tc] = val[q] * inv;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int a = q * 32 + (threadIdx.x >> 3), c8 = (threadIdx.x & 7) * 8;
+        if (r0 + a >= S) continue;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (tall ? tile[c8 + e][a] : tile[a][c8 + e]) * kUp;
+        store_factor(f, ((int64_t)i * S + r0 + a) * Lp + c0 + c8, x);
+    }
+}
+
+struct OrthOut {
+    int S, Sp, L, Lp;
+    Factors from, to;           // A or X that the step adds; A, B or the next X
+    // last step
+    int tall, update, out_bf16;
+    void* out;                  // M's place of the result, or X of the update
+    int64_t out_row, out_rep;
+    float lr, scale, wd;
+};
 
 template <typename S, BLayout LB, OrthStep STEP>
 __global__ void __launch_bounds__(S::kThreads) orth_product_kernel(TileArgs a, OrthOut o) {
@@ -269,6 +267,7 @@ struct Tiles {
     typedef TileShape<192, 192, 2, 4, 64, 1, 3> T192;
     typedef TileShape<128, 128, 2, 2, 64, 1, 2> T128;
     typedef TileShape<64, 64, 2, 2, 64, 1, 2> T64;
+    typedef TileShape<64, 64, 2, 2, 64, 1, 3, 2> T64Sym;
     static constexpr TileCost c256{27.f, 1.01f, 0.5f, 1, 1.f}, c192{18.f, 0.70f, 0.5f, 1, 1.f}, c128{12.f, 0.53f, 0.5f, 2, 1.25f},
         c64{3.3f, 0.45f, 0.15f, 5, 3.1f};
 };
@@ -278,18 +277,22 @@ struct Tiles<2> {
     typedef T256 T192;   // (192 rows of 32 k are no whole number of loads for 512 threads)
     typedef TileShape<128, 128, 2, 2, 32, 2, 2> T128;
     typedef TileShape<64, 64, 2, 2, 64, 2, 2> T64;
+    typedef TileShape<64, 64, 2, 2, 64, 2, 3, 2> T64Sym;
     static constexpr TileCost c256{23.5f, 3.17f, 0.5f, 1, 1.f}, c192 = c256, c128{10.3f, 1.58f, 0.5f, 2, 1.25f}, c64{3.2f, 0.60f, 0.15f, 2, 1.42f};
 };
 
 template <typename S>
-void launch_product(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t st) {
+void launch_symmetric(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t st) {
     const unsigned g = tile_grid<S>(a);
-    switch (step) {
-        case kGram: orth_product_kernel<S, KMajor, kGram><<<g, S::kThreads, 0, st>>>(a, o); break;
-        case kPoly: orth_product_kernel<S, KMajor, kPoly><<<g, S::kThreads, 0, st>>>(a, o); break;
-        case kNext: orth_product_kernel<S, NMajor, kNext><<<g, S::kThreads, 0, st>>>(a, o); break;
-        case kLast: orth_product_kernel<S, NMajor, kLast><<<g, S::kThreads, 0, st>>>(a, o); break;
-    }
+    if (step == kGram) orth_product_kernel<S, KMajor, kGram><<<g, S::kThreads, 0, st>>>(a, o);
+    else orth_product_kernel<S, KMajor, kPoly><<<g, S::kThreads, 0, st>>>(a, o);
+}
+template <typename S>
+void launch_product(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t st) {
+    if (step <= kPoly) return launch_symmetric<S>(a, o, step, st);
+    const unsigned g = tile_grid<S>(a);
+    if (step == kNext) orth_product_kernel<S, NMajor, kNext><<<g, S::kThreads, 0, st>>>(a, o);
+    else orth_product_kernel<S, NMajor, kLast><<<g, S::kThreads, 0, st>>>(a, o);
 }
 
 // The tile whose estimate is least.  Measured (us; 256, 192, 128, 64): 4096 x 4096 bf16, A: 112, 87, 113, 158, the next X:
@@ -308,7 +311,13 @@ void launch_step_parts(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t 
     const float t256 = cost(typename TT::T256(), TT::c256), t192 = cost(typename TT::T192(), TT::c192),
                 t128 = cost(typename TT::T128(), TT::c128), t64 = cost(typename TT::T64(), TT::c64);
     const float least = std::min(std::min(t256, t192), std::min(t128, t64));
-    if (t64 == least) launch_product<typename TT::T64>(a, o, step, st);
+    if (t64 == least) {
+        tile_grid<typename TT::T64>(a);
+        // not more tiles than compute units: two groups of wavefronts for each half of k and three buffers (768 x 3000 bf16, A:
+        // 25.7 and 18.0 us; 2 x 512 x 2048 fp32: 22.7 and 21.1); more: smaller workgroups, which share a unit (8 x 512 x 1024 fp32: 19 and 25)
+        if (step <= kPoly && (int64_t)a.per_batch * a.batches <= 256) launch_symmetric<typename TT::T64Sym>(a, o, step, st);
+        else launch_product<typename TT::T64>(a, o, step, st);
+    }
     else if (t128 == least) launch_product<typename TT::T128>(a, o, step, st);
     else if (t256 == least) launch_product<typename TT::T256>(a, o, step, st);
     else launch_product<typename TT::T192>(a, o, step, st);

@@ -72,18 +72,18 @@ enum BLayout { KMajor, NMajor, KMajorAny, NMajorAny };
 constexpr bool n_contiguous(BLayout l) { return l == NMajor || l == NMajorAny; }
 constexpr bool any_alignment(BLayout l) { return l == KMajorAny || l == NMajorAny; }
 
-template <int BM_, int BN_, int WM_, int WN_, int BK_, int NP_, int STAGES_>
+template <int BM_, int BN_, int WM_, int WN_, int BK_, int NP_, int STAGES_, int WK_ = 1>
 struct TileShape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;   // WM x WN wavefronts
-    static constexpr int BK = BK_, NP = NP_, KS = BK / 32;
-    static constexpr int kThreads = 64 * WM * WN;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WK = WK_;   // WM x WN wavefronts, each WK times: for its share of k
+    static constexpr int BK = BK_, NP = NP_, KS = BK / 32 / WK;
+    static constexpr int kThreads = 64 * WM * WN * WK;
     static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;     // 16 x 16 tiles of a wavefront
     static constexpr int kPart = (BM + BN) * BK;                   // elements of one part's tiles: A's, then B's
     static constexpr int kStage = NP * kPart;                      // ... of one LDS buffer
     static constexpr int kStages = STAGES_, kLds = kStages * kStage;
     static constexpr int kLoads = kStage / 8 / kThreads;           // load instructions of a thread for a buffer
     static_assert(kPart % (8 * kThreads) == 0 && kLoads * (kStages - 2) < 64, "what a wait can count");
-    static_assert(BM * BK % (8 * kThreads) == 0 && kLds * 2 <= 160 * 1024 && TM % 2 == 0, "");
+    static_assert(BM * BK % (8 * kThreads) == 0 && kLds * 2 <= 160 * 1024 && TM % 2 == 0 && (WK == 1 || BM * BN * 4 <= kLds * 2), "");
 };
 
 // What the place of a row's chunks (KMajor) or pairs (NMajor) is permuted with.
@@ -321,7 +321,7 @@ template <typename T, typename S, BLayout L>
 __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl, int kt0, int kt1, uint16_t* lds,
                                           f32x4 (&acc)[S::TM][S::TN]) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / S::WN, wn = wave % S::WN;
+    const int wk = S::WK == 1 ? 0 : wave / (S::WM * S::WN), wm = wave / S::WN - wk * S::WM, wn = wave % S::WN, ks0 = wk * S::KS;
     const int m0 = pl.tm * S::BM, n0 = pl.tn * S::BN, total = kt1 - kt0;
 #pragma unroll
     for (int i = 0; i < S::TM; ++i)
@@ -368,19 +368,23 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
     if constexpr (ANY) __builtin_amdgcn_s_waitcnt(kWaitLds);
     int buf = 0;
     // a quarter of the wavefront's tile at a time: half of its rows by half of its columns, all parts and 32-deep steps
-    constexpr int HM = S::TM / 2, NH = S::TN % 2 ? 1 : 2, HN = S::TN / NH;   // (an odd number of columns: half)
+    // (an odd number of columns: half; four 16 x 16 squares or fewer: all of it, so that consecutive products do not wait for
+    // each other's sums)
+    constexpr int MH = S::TM * S::TN <= 4 ? 1 : 2, HM = S::TM / MH, NH = MH == 1 || S::TN % 2 ? 1 : 2, HN = S::TN / NH;
+    constexpr bool TURNS = S::WM * S::WN == 8 && S::WK == 1;
+    static_assert(MH == 2 || !TURNS, "");
     s16x8 fa[HM][NP][KS], fb[NH][HN][NP][KS];
     auto read_b = [&](const uint16_t* tb, int h) {
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+            for (int p = 0; p < NP; ++p)
 #pragma unroll
                 for (int j = 0; j < HN; ++j) {
                     if constexpr (!n_contiguous(L))
-                        fb[h][j][p][ks] = read_kmajor<S::BK>(tb + p * S::kPart, (wn * S::TN + h * HN + j) * 16, ks, lane);
+                        fb[h][j][p][ks] = read_kmajor<S::BK>(tb + p * S::kPart, (wn * S::TN + h * HN + j) * 16, ks0 + ks, lane);
                     else
-                        fb[h][j][p][ks] = read_nmajor<S::BN>(tb + p * S::kPart, (wn * S::TN + h * HN + j) * 16, ks, lane);
+                        fb[h][j][p][ks] = read_nmajor<S::BN>(tb + p * S::kPart, (wn * S::TN + h * HN + j) * 16, ks0 + ks, lane);
                 }
     };
     auto read_a = [&](const uint16_t* ta, int h) {
@@ -389,7 +393,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int i = 0; i < HM; ++i) fa[i][p][ks] = read_kmajor<S::BK>(ta + p * S::kPart, (wm * S::TM + h * HM + i) * 16, ks, lane);
+                for (int i = 0; i < HM; ++i) fa[i][p][ks] = read_kmajor<S::BK>(ta + p * S::kPart, (wm * S::TM + h * HM + i) * 16, ks0 + ks, lane);
     };
     auto mma = [&](int hm, int hn) {
 #pragma unroll
@@ -416,7 +420,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         if (asked == NS - 2) __builtin_amdgcn_s_waitcnt(wait_loads((NS - 2) * kCounted));
         else __builtin_amdgcn_s_waitcnt(wait_loads(0));
     };
-    if constexpr (S::WM * S::WN == 8) {
+    if constexpr (TURNS) {
         const bool late = wave >= 4;
         oldest(ahead - 1);
         tile_barrier();
@@ -449,27 +453,62 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         }
         if (!late) tile_barrier();
     } else {
+        // what is in LDS is asked for before the next tile: the compiler otherwise reads it piece by piece, each with its wait
+        // (8 x 100 rows, 512 x 20000 in fp32: 242 and 186 us).  With two buffers the next tile is already late, and with rows
+        // of k the reads cost more than their order gives (4 x 1000 x 2000 bf16: 25.1 and 27.6 us).
+        constexpr bool kReadFirst = n_contiguous(L) || NS > 2;
         for (int t = 0; t < total; ++t) {
             oldest(min(total - t, NS - 1) - 1);
             tile_barrier();   // the tile is there, and all have read the one whose place is filled next
             const uint16_t *ta = lds + buf * S::kStage, *tb = ta + S::BM * S::BK;
             buf = buf + 1 == NS ? 0 : buf + 1;
-            if (t + NS - 1 < total) {
+            const bool more = t + NS - 1 < total;
+            if (!kReadFirst && more) {
                 ask_a();
                 ask_b();
             }
             read_b(tb, 0);
             read_a(ta, 0);
             if constexpr (NH == 2) read_b(tb, 1);
+            if constexpr (kReadFirst) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (more) {
+                    ask_a();
+                    ask_b();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
             mma(0, 0);
             if constexpr (NH == 2) mma(0, 1);
-            read_a(ta, 1);
-            if constexpr (NH == 2) mma(1, 1);
-            mma(1, 0);
-            if (t + NS - 1 < total) commit_b();
+            if constexpr (MH == 2) {
+                read_a(ta, 1);
+                if constexpr (NH == 2) mma(1, 1);
+                mma(1, 0);
+            }
+            if (more) commit_b();
             __builtin_amdgcn_s_waitcnt(kWaitLds);
         }
         tile_barrier();
+    }
+    if constexpr (S::WK > 1) {   // the shares' sums, in the order of k
+        f32x4* at = reinterpret_cast<f32x4*>(lds) + (wave % (S::WM * S::WN) * S::TM * S::TN) * 64 + lane;
+#pragma unroll
+        for (int w = 1; w < S::WK; ++w) {
+            if (wk == w) {
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::TN; ++j) at[(i * S::TN + j) * 64] = acc[i][j];
+            }
+            __syncthreads();
+            if (wk == 0) {
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::TN; ++j) acc[i][j] += at[(i * S::TN + j) * 64];
+            }
+            if (w + 1 < S::WK) __syncthreads();
+        }
     }
 }
 
@@ -497,6 +536,7 @@ struct SumSlices {
     __device__ __forceinline__ void put(const f32x4 (&acc)[S::TM][S::TN]) const {
         const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w / S::WN, wn = w % S::WN;
         __syncthreads();
+        if (S::WK == 1 || w < S::WM * S::WN)
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
 #pragma unroll
