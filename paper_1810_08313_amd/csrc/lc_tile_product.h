@@ -184,48 +184,59 @@ __device__ __forceinline__ s16x8 read_nmajor(const uint16_t* tile, int col, int 
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// The same through registers: load() asks, commit() writes to LDS what has come.  `len` is any length of at least 8.
+// The same through registers: load() asks, commit() writes to LDS what has come.  `len` is any length of at least 8.  What
+// the end of a row cuts off is loaded as the row's last 8 and moved in registers (element by element, that one tile of each row
+// of tiles held up the others: 1 row, 2048 x 50257, 87 us and 49).
 template <int R, int BK, int THREADS, bool NMAJOR>
 struct AnyFetch {
     static constexpr int kAcross = NMAJOR ? R : BK, kChunks = kAcross / 8, kPer = THREADS / kChunks, kLoads = (NMAJOR ? BK : R) / kPer;
     u32x4 reg[kLoads];
     int r0, x0, c;   // the lane's row (and chunk) inside the tile; the chunk's first place
-    __device__ __forceinline__ void init(const TileOperand&, int first) {
+    int left;        // of the row, from the tile's first place on
+    uint32_t off[kLoads];   // bytes: NMAJOR as in NMajorFetch, otherwise of the row from the tile's first
+    __device__ __forceinline__ void init(const TileOperand& o, int first) {
         const int t = threadIdx.x;
         r0 = t / kChunks;
         x0 = first;
         c = t % kChunks;
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) {
+            const int r = q * kPer + r0, row = NMAJOR ? r : min(x0 + r, o.rows - 1) - x0;
+            off[q] = ((uint32_t)row * (uint32_t)o.row + (NMAJOR ? (uint32_t)min(x0 + place(q), o.len - 8) : 0u)) * 2u;
+        }
+    }
+    __device__ __forceinline__ int place(int q) const {   // of a chunk's first element in the tile's row
+        const int r = q * kPer + r0;
+        return (NMAJOR ? c ^ n_place<R>(r) << 1 : c ^ k_place<BK>(r)) * 8;
     }
     // `base`: the operand's first element (NMAJOR), or the tile's first row
     __device__ __forceinline__ void load(const TileOperand& o, const char* base, int k0) {
+        left = o.len - (NMAJOR ? x0 : k0);
+        const int last = o.rows - 1;
+        const uint32_t row2 = (uint32_t)o.row * 2u;
+        const char* at = NMAJOR ? base + (int64_t)min(k0, last) * row2 : base;
+        const bool more = NMAJOR && k0 + BK > o.rows;   // rows behind the last: that one
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
-            const int r = q * kPer + r0;
-            int row, x;
-            if constexpr (NMAJOR) {
-                row = min(k0 + r, o.rows - 1);
-                x = x0 + (c ^ n_place<R>(r) << 1) * 8;
-            } else {
-                row = min(x0 + r, o.rows - 1) - x0;
-                x = k0 + (c ^ k_place<BK>(r)) * 8;
-            }
-            const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + (int64_t)row * o.row;
-            if (x + 8 <= o.len) {
-                __builtin_memcpy(&reg[q], p + x, 16);
-            } else {
-                uint32_t w[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t lo = x + 2 * e < o.len ? p[x + 2 * e] : 0, hi = x + 2 * e + 1 < o.len ? p[x + 2 * e + 1] : 0;
-                    w[e] = lo | hi << 16;
-                }
-                reg[q] = u32x4{w[0], w[1], w[2], w[3]};
-            }
+            uint32_t d = off[q];
+            if constexpr (!NMAJOR) d += 2u * (uint32_t)min(k0 + place(q), o.len - 8);
+            else if (more) d -= (uint32_t)(q * kPer + r0 - (min(k0 + q * kPer + r0, last) - min(k0, last))) * row2;
+            __builtin_memcpy(&reg[q], at + d, 16);
         }
     }
     __device__ __forceinline__ void commit(uint16_t* to) const {
 #pragma unroll
-        for (int q = 0; q < kLoads; ++q) *reinterpret_cast<u32x4*>(to + (q * THREADS + threadIdx.x) * 8) = reg[q];
+        for (int q = 0; q < kLoads; ++q) {
+            u32x4 w = reg[q];
+            if (left < kAcross) {
+                const int cut = min(max(place(q) + 8 - left, 0), 8);   // elements in front of the chunk; zeros follow
+                const uint32_t a0 = cut & 4 ? w[2] : w[0], a1 = cut & 4 ? w[3] : w[1], a2 = cut & 4 ? 0 : w[2], a3 = cut & 4 ? 0 : w[3];
+                const uint32_t b0 = cut & 2 ? a1 : a0, b1 = cut & 2 ? a2 : a1, b2 = cut & 2 ? a3 : a2, b3 = cut & 2 ? 0 : a3, s = (cut & 1) * 16;
+                w = cut == 8 ? u32x4{0, 0, 0, 0}
+                             : u32x4{__builtin_amdgcn_alignbit(b1, b0, s), __builtin_amdgcn_alignbit(b2, b1, s), __builtin_amdgcn_alignbit(b3, b2, s), b3 >> s};
+            }
+            *reinterpret_cast<u32x4*>(to + (q * THREADS + threadIdx.x) * 8) = w;
+        }
     }
 };
 
@@ -337,7 +348,9 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
     constexpr int NS = S::kStages, NP = S::NP, KS = S::KS;
     constexpr bool ANY = any_alignment(L);
     static_assert(!ANY || NP == 1, "");
-    constexpr int kCounted = ANY ? S::BM * S::BK / 8 / S::kThreads : S::kLoads;   // loads of a tile that go straight into LDS
+    // What comes through registers is written to LDS at the end of the k tile that asked for it, or, with three buffers, in
+    // the middle of the next (8 x 128 rows, 512 x 50257, dA: 149 and 130 us).  Loads return in order: its A is there, too.
+    constexpr bool kLate = ANY && NS > 2;
     int next_k = kt0 * S::BK, next_buf = 0;   // of the tile that is fetched next
     auto ask_a = [&] {
 #pragma unroll
@@ -357,7 +370,10 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         next_buf = next_buf + 1 == NS ? 0 : next_buf + 1;
     };
     auto commit_b = [&] {
-        if constexpr (ANY) fetch_b.commit(pending);
+        if constexpr (ANY) {
+            if (pending) fetch_b.commit(pending);
+            pending = nullptr;
+        }
     };
     const int ahead = min(NS - 1, total);
     for (int t = 0; t < ahead; ++t) {
@@ -365,7 +381,10 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         ask_b();
         commit_b();
     }
-    if constexpr (ANY) __builtin_amdgcn_s_waitcnt(kWaitLds);
+    if constexpr (ANY) {
+        __builtin_amdgcn_s_waitcnt(wait_loads(0));
+        __builtin_amdgcn_s_waitcnt(kWaitLds);
+    }
     int buf = 0;
     // a quarter of the wavefront's tile at a time: half of its rows by half of its columns, all parts and 32-deep steps
     // (an odd number of columns: half; four 16 x 16 squares or fewer: all of it, so that consecutive products do not wait for
@@ -417,7 +436,8 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         tile_barrier();
     };
     auto oldest = [&](int asked) {   // tiles asked for beyond the one that is waited for
-        if (asked == NS - 2) __builtin_amdgcn_s_waitcnt(wait_loads((NS - 2) * kCounted));
+        if constexpr (kLate) return;
+        if (asked == NS - 2) __builtin_amdgcn_s_waitcnt(wait_loads((NS - 2) * S::kLoads));
         else __builtin_amdgcn_s_waitcnt(wait_loads(0));
     };
     if constexpr (TURNS) {
@@ -435,18 +455,20 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
             if constexpr (NH == 2) {
                 turn(0, 0);
                 read_b(tb, 1);
+                if (kLate) commit_b();
                 if (more) ask_b();
                 turn(0, 1);
                 read_a(ta, 1);
                 turn(1, 1);
-                if (more) commit_b();
+                if (!kLate) commit_b();
                 oldest(more ? NS - 2 : 0);
                 turn(1, 0);
             } else {
+                if (kLate) commit_b();
                 if (more) ask_b();
                 turn(0, 0);
                 read_a(ta, 1);
-                if (more) commit_b();
+                if (!kLate) commit_b();
                 oldest(more ? NS - 2 : 0);
                 turn(1, 0);
             }
@@ -464,6 +486,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
             buf = buf + 1 == NS ? 0 : buf + 1;
             const bool more = t + NS - 1 < total;
             if (!kReadFirst && more) {
+                static_assert(!kLate || kReadFirst, "");
                 ask_a();
                 ask_b();
             }
@@ -472,6 +495,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
             if constexpr (NH == 2) read_b(tb, 1);
             if constexpr (kReadFirst) {
                 __builtin_amdgcn_sched_barrier(0);
+                if (kLate) commit_b();
                 if (more) {
                     ask_a();
                     ask_b();
@@ -485,7 +509,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
                 if constexpr (NH == 2) mma(1, 1);
                 mma(1, 0);
             }
-            if (more) commit_b();
+            if (!kLate) commit_b();
             __builtin_amdgcn_s_waitcnt(kWaitLds);
         }
         tile_barrier();
