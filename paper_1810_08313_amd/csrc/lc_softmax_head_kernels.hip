@@ -30,17 +30,6 @@ constexpr int kBlock = 256;
 constexpr int64_t kKeepBytes = 2147483648LL;      // of e, and what stands beside it, at a time
 constexpr float kEScale = 32768.f, kEShift = 15.f;   // 2^15
 
-__device__ __forceinline__ uint16_t bits(bf16_t x) { return __builtin_bit_cast(uint16_t, x); }
-// x as the sum of three bf16 (24 bits: exact unless the last parts leave the exponent range).
-__device__ __forceinline__ void split3(float x, uint16_t (&p)[3]) {
-    const bf16_t a = static_cast<bf16_t>(x);
-    const float r = x - static_cast<float>(a);
-    const bf16_t b = static_cast<bf16_t>(r);
-    p[0] = bits(a);
-    p[1] = bits(b);
-    p[2] = bits(static_cast<bf16_t>(r - static_cast<float>(b)));
-}
-
 // ------------------------------------------------------------------ kept rows
 
 // order[0 .. kept): rows that count, in their order; behind them the others, whose loss is zero.
@@ -707,6 +696,18 @@ int head_wide(const lc_head_args& h) {
     return h.rows > 64 || (int64_t)h.m * ((h.classes + 255) / 256) < 256 ? 128 : 256;
 }
 
+// fp32 weights are split in every product, of the products' own time, up to so many rows; for more they are copied in parts
+// first, which writes 6 bytes a weight (4 x 512 x 20001: 64 us) and reads them in each product.  All of a call without and with
+// a copy, us: 4 x 60 rows, loss: 98, 163, gradients: 254, 358; 4 x 512: 288, 344 and 1021, 1050; 1 x 2048, 1024 x 20000: 579,
+// 554 and 1626, 1646; 8192: 2009, 1899 and 5842, 5715.  Few weights, or few workgroups for them, are copied in less than the
+// loads' detour through registers costs each of a workgroup's k tiles: 8 x 60 rows, 512 x 1000: 67, 65; 512 x 2000: 85, 92;
+// 2 x 60, 2048 x 2000: 146, 138.
+constexpr int kSplitRows = 512, kSplitWorkgroups = 64;
+constexpr int64_t kSplitWeights = 6 << 20;
+bool split_in_place(const lc_head_args& h, int parts) {
+    return h.rows <= kSplitRows && (int64_t)h.m * parts >= kSplitWorkgroups && (int64_t)h.m * h.inputs * h.classes >= kSplitWeights;
+}
+
 int copy_across(int cp) { return std::min((cp + kBlock * 8 - 1) / (kBlock * 8), 64); }
 
 struct HeadPlan {
@@ -760,9 +761,8 @@ HeadPlan head_plan(const lc_head_args& h, bool grad, void* ws) {
     p.ep = round_up(h.classes, kPadK);
     // bf16 weights are read where they stand: straight into LDS if every row starts on 16 bytes and holds whole chunks of 8,
     // through registers otherwise (8 x 128 rows, 512 x 50257: a copy first cost 207 us of 860)
-    p.any_w = !p.three && (h.classes % 8 || !aligned_to(h.W.p, 16) || (h.inputs > 1 && h.W.row % 8) || (h.m > 1 && h.W.replica % 8));
-    p.copy_w = p.three || h.classes < 8 || (h.inputs > 1 && h.W.row > kMaxRowStride);
-    if (p.copy_w) p.any_w = false;
+    p.copy_w = (p.three && !split_in_place(h, p.parts)) || h.classes < 8 || (h.inputs > 1 && h.W.row > kMaxRowStride / (p.three ? 2 : 1));
+    p.any_w = !p.copy_w && (p.three || h.classes % 8 || !aligned_to(h.W.p, 16) || (h.inputs > 1 && h.W.row % 8) || (h.m > 1 && h.W.replica % 8));
     p.cp = static_cast<int>(round_up(h.classes, 8));
     // rows and replicas at a time: bytes of a row's e (fp32: and of its dZ in parts), or of its parts' sums
     const int64_t per_row = grad ? p.ep * (p.three ? 10 : 2) : p.parts * 8;
@@ -873,13 +873,8 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             if (here) {
                 auto logits = [&](auto s) {
                     typedef decltype(s) S;
-                    if constexpr (sizeof(T) == 2) {
-                        if (p.any_w) {
-                            head_logits_kernel<S, E, NMajorAny><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, l);
-                            return;
-                        }
-                    }
-                    head_logits_kernel<S, E, NMajor><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, l);
+                    if (p.any_w) head_logits_kernel<S, E, NMajorAny><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, l);
+                    else head_logits_kernel<S, E, NMajor><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, l);
                 };
                 if (p.wide == 128 && rows <= 64) logits(typename Tiles<sizeof(T) == 4>::Few());
                 else if (p.wide == 128) logits(typename Tiles<sizeof(T) == 4>::Half());
@@ -931,23 +926,14 @@ int run_head(const lc_head_args& h, const HeadPlan& p, hipStream_t st) {
             const int n_rows = static_cast<int>(n);
             if (here && da_blocks + dw_blocks <= kBothGrads) {
                 const unsigned grid = da_blocks + dw_blocks;
-                if constexpr (sizeof(T) == 2) {
-                    if (p.any_w) head_grads_kernel<Small, KMajorAny, G><<<grid, Small::kThreads, 0, st>>>(t, p.da, n_rows, p.d4, da_blocks, u, dw);
-                    else head_grads_kernel<Small, KMajor, G><<<grid, Small::kThreads, 0, st>>>(t, p.da, n_rows, p.d4, da_blocks, u, dw);
-                } else {
-                    head_grads_kernel<Small, KMajor, G><<<grid, Small::kThreads, 0, st>>>(t, p.da, n_rows, p.d4, da_blocks, u, dw);
-                }
+                if (p.any_w) head_grads_kernel<Small, KMajorAny, G><<<grid, Small::kThreads, 0, st>>>(t, p.da, n_rows, p.d4, da_blocks, u, dw);
+                else head_grads_kernel<Small, KMajor, G><<<grid, Small::kThreads, 0, st>>>(t, p.da, n_rows, p.d4, da_blocks, u, dw);
             } else {
                 if (here)
                     with_tile<sizeof(T) == 4>(t, [&](auto s) {
                         typedef decltype(s) S;
-                        if constexpr (sizeof(T) == 2) {
-                            if (p.any_w) {
-                                head_da_kernel<S, KMajorAny><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, p.da, n_rows, p.d4);
-                                return;
-                            }
-                        }
-                        head_da_kernel<S, KMajor><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, p.da, n_rows, p.d4);
+                        if (p.any_w) head_da_kernel<S, KMajorAny><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, p.da, n_rows, p.d4);
+                        else head_da_kernel<S, KMajor><<<tile_grid<S>(t), S::kThreads, 0, st>>>(t, p.da, n_rows, p.d4);
                     });
                 with_tile<sizeof(T) == 4>(u, [&](auto s) {
                     typedef decltype(s) S;

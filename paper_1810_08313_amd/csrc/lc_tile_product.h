@@ -67,10 +67,21 @@ struct TileArgs {
 };
 
 // ...Any: rows that start anywhere and hold any number of elements; they come through registers, since what goes
-// straight into LDS has to be aligned.
+// straight into LDS has to be aligned.  With three parts the elements are floats, split on the way.
 enum BLayout { KMajor, NMajor, KMajorAny, NMajorAny };
 constexpr bool n_contiguous(BLayout l) { return l == NMajor || l == NMajorAny; }
 constexpr bool any_alignment(BLayout l) { return l == KMajorAny || l == NMajorAny; }
+
+__device__ __forceinline__ uint16_t bits(bf16_t x) { return __builtin_bit_cast(uint16_t, x); }
+// x as the sum of three bf16 (24 bits: exact unless the last parts leave the exponent range).
+__device__ __forceinline__ void split3(float x, uint16_t (&p)[3]) {
+    const bf16_t a = static_cast<bf16_t>(x);
+    const float r = x - static_cast<float>(a);
+    const bf16_t b = static_cast<bf16_t>(r);
+    p[0] = bits(a);
+    p[1] = bits(b);
+    p[2] = bits(static_cast<bf16_t>(r - static_cast<float>(b)));
+}
 
 template <int BM_, int BN_, int WM_, int WN_, int BK_, int NP_, int STAGES_, int WK_ = 1>
 struct TileShape {
@@ -187,10 +198,12 @@ __device__ __forceinline__ s16x8 read_nmajor(const uint16_t* tile, int col, int 
 // The same through registers: load() asks, commit() writes to LDS what has come.  `len` is any length of at least 8.  What
 // the end of a row cuts off is loaded as the row's last 8 and moved in registers (element by element, that one tile of each row
 // of tiles held up the others: 1 row, 2048 x 50257, 87 us and 49).
-template <int R, int BK, int THREADS, bool NMAJOR>
+template <int R, int BK, int THREADS, bool NMAJOR, int NP>
 struct AnyFetch {
+    static_assert(NP == 1 || NP == 3, "");
+    static constexpr uint32_t kBytes = NP == 1 ? 2 : 4;   // of an element
     static constexpr int kAcross = NMAJOR ? R : BK, kChunks = kAcross / 8, kPer = THREADS / kChunks, kLoads = (NMAJOR ? BK : R) / kPer;
-    u32x4 reg[kLoads];
+    u32x4 reg[kLoads][kBytes / 2];
     int r0, x0, c;   // the lane's row (and chunk) inside the tile; the chunk's first place
     int left;        // of the row, from the tile's first place on
     uint32_t off[kLoads];   // bytes: NMAJOR as in NMajorFetch, otherwise of the row from the tile's first
@@ -202,7 +215,7 @@ struct AnyFetch {
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
             const int r = q * kPer + r0, row = NMAJOR ? r : min(x0 + r, o.rows - 1) - x0;
-            off[q] = ((uint32_t)row * (uint32_t)o.row + (NMAJOR ? (uint32_t)min(x0 + place(q), o.len - 8) : 0u)) * 2u;
+            off[q] = ((uint32_t)row * (uint32_t)o.row + (NMAJOR ? (uint32_t)min(x0 + place(q), o.len - 8) : 0u)) * kBytes;
         }
     }
     __device__ __forceinline__ int place(int q) const {   // of a chunk's first element in the tile's row
@@ -213,29 +226,58 @@ struct AnyFetch {
     __device__ __forceinline__ void load(const TileOperand& o, const char* base, int k0) {
         left = o.len - (NMAJOR ? x0 : k0);
         const int last = o.rows - 1;
-        const uint32_t row2 = (uint32_t)o.row * 2u;
-        const char* at = NMAJOR ? base + (int64_t)min(k0, last) * row2 : base;
+        const uint32_t row_bytes = (uint32_t)o.row * kBytes;
+        const char* at = NMAJOR ? base + (int64_t)min(k0, last) * row_bytes : base;
         const bool more = NMAJOR && k0 + BK > o.rows;   // rows behind the last: that one
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
             uint32_t d = off[q];
-            if constexpr (!NMAJOR) d += 2u * (uint32_t)min(k0 + place(q), o.len - 8);
-            else if (more) d -= (uint32_t)(q * kPer + r0 - (min(k0 + q * kPer + r0, last) - min(k0, last))) * row2;
-            __builtin_memcpy(&reg[q], at + d, 16);
+            if constexpr (!NMAJOR) d += kBytes * (uint32_t)min(k0 + place(q), o.len - 8);
+            else if (more) d -= (uint32_t)(q * kPer + r0 - (min(k0 + q * kPer + r0, last) - min(k0, last))) * row_bytes;
+            __builtin_memcpy(&reg[q], at + d, 8 * kBytes);
         }
     }
-    __device__ __forceinline__ void commit(uint16_t* to) const {
+    // elements in front of chunk q of what was loaded for it; zeros follow
+    __device__ __forceinline__ int cut(int q) const { return min(max(place(q) + 8 - left, 0), 8); }
+    __device__ __forceinline__ void commit(uint16_t* to, int part) const {
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
-            u32x4 w = reg[q];
-            if (left < kAcross) {
-                const int cut = min(max(place(q) + 8 - left, 0), 8);   // elements in front of the chunk; zeros follow
-                const uint32_t a0 = cut & 4 ? w[2] : w[0], a1 = cut & 4 ? w[3] : w[1], a2 = cut & 4 ? 0 : w[2], a3 = cut & 4 ? 0 : w[3];
-                const uint32_t b0 = cut & 2 ? a1 : a0, b1 = cut & 2 ? a2 : a1, b2 = cut & 2 ? a3 : a2, b3 = cut & 2 ? 0 : a3, s = (cut & 1) * 16;
-                w = cut == 8 ? u32x4{0, 0, 0, 0}
-                             : u32x4{__builtin_amdgcn_alignbit(b1, b0, s), __builtin_amdgcn_alignbit(b2, b1, s), __builtin_amdgcn_alignbit(b3, b2, s), b3 >> s};
+            uint16_t* at = to + (q * THREADS + threadIdx.x) * 8;
+            if constexpr (NP == 1) {
+                u32x4 w = reg[q][0];
+                if (left < kAcross) {
+                    const int n = cut(q);
+                    const uint32_t a0 = n & 4 ? w[2] : w[0], a1 = n & 4 ? w[3] : w[1], a2 = n & 4 ? 0 : w[2], a3 = n & 4 ? 0 : w[3];
+                    const uint32_t b0 = n & 2 ? a1 : a0, b1 = n & 2 ? a2 : a1, b2 = n & 2 ? a3 : a2, b3 = n & 2 ? 0 : a3, s = (n & 1) * 16;
+                    w = n == 8 ? u32x4{0, 0, 0, 0}
+                               : u32x4{__builtin_amdgcn_alignbit(b1, b0, s), __builtin_amdgcn_alignbit(b2, b1, s), __builtin_amdgcn_alignbit(b3, b2, s), b3 >> s};
+                }
+                *reinterpret_cast<u32x4*>(at) = w;
+            } else {
+                float v[8];
+                __builtin_memcpy(v, &reg[q], 32);
+                if (left < kAcross) {
+                    const int n = cut(q);
+#pragma unroll
+                    for (int step = 4; step > 0; step >>= 1)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float far = e + step < 8 ? v[e + step < 8 ? e + step : 7] : 0.f, near = v[e];
+                            v[e] = n & step ? far : near;
+                        }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = n == 8 ? 0.f : v[e];
+                }
+                s16x8 h[3];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    uint16_t p[3];
+                    split3(v[e], p);
+                    h[0][e] = (short)p[0]; h[1][e] = (short)p[1]; h[2][e] = (short)p[2];
+                }
+#pragma unroll
+                for (int p = 0; p < 3; ++p) *reinterpret_cast<s16x8*>(at + p * part) = h[p];
             }
-            *reinterpret_cast<u32x4*>(to + (q * THREADS + threadIdx.x) * 8) = w;
         }
     }
 };
@@ -250,11 +292,11 @@ struct FetchB<NMajor, S> {
 };
 template <typename S>
 struct FetchB<KMajorAny, S> {
-    typedef AnyFetch<S::BN, S::BK, S::kThreads, false> type;
+    typedef AnyFetch<S::BN, S::BK, S::kThreads, false, S::NP> type;
 };
 template <typename S>
 struct FetchB<NMajorAny, S> {
-    typedef AnyFetch<S::BN, S::BK, S::kThreads, true> type;
+    typedef AnyFetch<S::BN, S::BK, S::kThreads, true, S::NP> type;
 };
 
 struct TilePlace {
@@ -340,14 +382,14 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
         for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (total <= 0) return;
     const char* ab = reinterpret_cast<const char*>(a.a.p + (int64_t)pl.batch * a.a.batch + (int64_t)m0 * a.a.row);
-    const char* bb = reinterpret_cast<const char*>(a.b.p + (int64_t)pl.batch * a.b.batch + (n_contiguous(L) ? 0 : (int64_t)n0 * a.b.row));
+    const char* bb = reinterpret_cast<const char*>(a.b.p) + ((int64_t)pl.batch * a.b.batch + (n_contiguous(L) ? 0 : (int64_t)n0 * a.b.row)) *
+                                                                (any_alignment(L) && S::NP == 3 ? 4 : 2);
     KMajorFetch<S::BM, S::BK, S::kThreads> fetch_a;
     typename FetchB<L, S>::type fetch_b;
     fetch_a.init(a.a, m0);
     fetch_b.init(a.b, n0);
     constexpr int NS = S::kStages, NP = S::NP, KS = S::KS;
     constexpr bool ANY = any_alignment(L);
-    static_assert(!ANY || NP == 1, "");
     // What comes through registers is written to LDS at the end of the k tile that asked for it, or, with three buffers, in
     // the middle of the next (8 x 128 rows, 512 x 50257, dA: 149 and 130 us).  Loads return in order: its A is there, too.
     constexpr bool kLate = ANY && NS > 2;
@@ -371,7 +413,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const TilePlace pl,
     };
     auto commit_b = [&] {
         if constexpr (ANY) {
-            if (pending) fetch_b.commit(pending);
+            if (pending) fetch_b.commit(pending, S::kPart);
             pending = nullptr;
         }
     };

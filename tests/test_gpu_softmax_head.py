@@ -347,3 +347,45 @@ def test_more_replicas_than_a_launch_has_threads_for(pkg):
         _check("db", db[i], want["db"], want["db_tol"])
     ref = torch.nn.functional.cross_entropy((A[:, 0, :, None] * W).sum(1) + b, y[:, 0].long(), reduction="none")
     assert torch.allclose(loss, ref, rtol=1e-3, atol=1e-3)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("rows", [1, 70, 300, 520])
+def test_what_stands_between_rows_of_the_weights_is_not_used(pkg, bf16, rows):
+    """Every length of a row's end, rows of W at odd distances with NaN between and around them."""
+    import torch
+    m, d = 2, 45
+    for k, classes in enumerate((8, 9, 15, 23, 31, 33, 63, 66, 127, 129, 130, 255, 259, 268)):
+        A, W, b, y = _inputs(m, rows, d, classes, bf16, 50 + k, 0.1)
+        off, row = 1 + k % 8, classes + 1 + k % 5
+        P = torch.full((m, off + d * row + 16), float("nan"), device="cuda", dtype=W.dtype)
+        Wv = P.as_strided((m, d, classes), (P.stride(0), row, 1), off)
+        Wv.copy_(W)
+        loss, row_loss = pkg.softmax_head_loss(A, Wv, b, y)
+        _check_all(A, W, b, y, loss, row_loss)
+        loss, dA, dW, db = pkg.softmax_head_grad(A, Wv, b, y)
+        _check_all(A, W, b, y, loss, None, (dA, dW, db))
+
+
+def test_shared_fp32_weights(pkg):
+    A, W, b, y = _inputs(3, 40, 64, 520, False, 14)
+    Ws, bs = W[:1].expand(3, 64, 520), b[:1].expand(3, 520)
+    loss, dA, dW, db = pkg.softmax_head_grad(A, Ws, bs, y)
+    _check_all(A, Ws, bs, y, loss, None, (dA, dW, db))
+
+
+@pytest.mark.parametrize("rows", [1, 66, 300])
+def test_fp32_weights_split_on_their_way(pkg, rows):
+    """As many weights as that is done for, at every alignment of 4 bytes."""
+    import torch
+    m, d = 5, 130
+    for k, classes in enumerate((10000, 10001, 10003, 10126)):
+        A, W, b, y = _inputs(m, rows, d, classes, False, 70 + k, 0.1)
+        row = classes + k
+        P = torch.full((m, 16 + d * row), float("nan"), device="cuda")
+        Wv = P.as_strided((m, d, classes), (P.stride(0), row, 1), 1 + k)
+        Wv.copy_(W)
+        loss, row_loss = pkg.softmax_head_loss(A, Wv, b, y)
+        _check_all(A, W, b, y, loss, row_loss)
+        loss, dA, dW, db = pkg.softmax_head_grad(A, Wv, b, y)
+        _check_all(A, W, b, y, loss, None, (dA, dW, db))
