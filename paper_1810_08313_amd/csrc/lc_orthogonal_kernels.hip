@@ -161,13 +161,54 @@ struct OrthOut {
     float lr, scale, wd;
 };
 
-template <typename S, BLayout LB, OrthStep STEP>
-__global__ void __launch_bounds__(S::kThreads) orth_product_kernel(TileArgs a, OrthOut o) {
+// A tile's place in a workspace of sums in the order that wavefronts hold them: [share of k][matrix][tile].
+template <typename S>
+__device__ __forceinline__ f32x4* sums_of(float* part, const TileArgs& a, const TilePlace& pl, int split) {
+    const int64_t tile = ((int64_t)split * a.batches + pl.batch) * a.per_batch + pl.tile;
+    return reinterpret_cast<f32x4*>(part + tile * S::BM * S::BN) + threadIdx.x / 64 * (S::TM * S::TN * 64) + threadIdx.x % 64;
+}
+
+// One share of k of a symmetric product.
+template <typename S>
+__global__ void __launch_bounds__(S::kThreads) orth_share_kernel(TileArgs a, float* part) {
+    __shared__ __align__(1024) uint16_t lds[S::kLds];
+    const TilePlace pl = tile_place<S>(a, blockIdx.x);
+    if (pl.batch < 0) return;
+    int k0, k1;
+    tile_k_range<S>(a, pl, k0, k1);
+    f32x4 acc[S::TM][S::TN];
+    tile_sums<f16_t, S, KMajor>(a, pl, k0, k1, lds, acc);
+    if (threadIdx.x >= S::kThreads / S::WK) return;
+    f32x4* to = sums_of<S>(part, a, pl, pl.split);
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) to[(i * S::TN + j) * 64] = acc[i][j];
+}
+
+// SHARES: of `shares` such sums, added up in the order of k.
+template <typename S, BLayout LB, OrthStep STEP, bool SHARES = false>
+__global__ void __launch_bounds__(S::kThreads) orth_product_kernel(TileArgs a, OrthOut o, float* part, int shares) {
     __shared__ __align__(1024) uint16_t lds[S::kLds];
     const TilePlace pl = tile_place<S>(a, blockIdx.x);
     if (pl.batch < 0) return;
     f32x4 acc[S::TM][S::TN];
-    tile_sums<f16_t, S, LB>(a, pl, 0, a.K / S::BK, lds, acc);
+    if constexpr (SHARES) {
+        const f32x4* from = sums_of<S>(part, a, pl, 0);
+        const int64_t next = (int64_t)a.batches * a.per_batch * (S::BM * S::BN / 4);
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) acc[i][j] = from[(i * S::TN + j) * 64];
+#pragma unroll 4
+        for (int k = 1; k < shares; ++k)
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j) acc[i][j] += from[k * next + (i * S::TN + j) * 64];
+    } else {
+        tile_sums<f16_t, S, LB>(a, pl, 0, a.K / S::BK, lds, acc);
+    }
     const int m0 = pl.tm * S::BM, n0 = pl.tn * S::BN;
     const SumSlices<S> sums(lds);
     each_slice<S>([&](auto slice) {
@@ -284,15 +325,15 @@ struct Tiles<2> {
 template <typename S>
 void launch_symmetric(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t st) {
     const unsigned g = tile_grid<S>(a);
-    if (step == kGram) orth_product_kernel<S, KMajor, kGram><<<g, S::kThreads, 0, st>>>(a, o);
-    else orth_product_kernel<S, KMajor, kPoly><<<g, S::kThreads, 0, st>>>(a, o);
+    if (step == kGram) orth_product_kernel<S, KMajor, kGram><<<g, S::kThreads, 0, st>>>(a, o, nullptr, 0);
+    else orth_product_kernel<S, KMajor, kPoly><<<g, S::kThreads, 0, st>>>(a, o, nullptr, 0);
 }
 template <typename S>
 void launch_product(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t st) {
     if (step <= kPoly) return launch_symmetric<S>(a, o, step, st);
     const unsigned g = tile_grid<S>(a);
-    if (step == kNext) orth_product_kernel<S, NMajor, kNext><<<g, S::kThreads, 0, st>>>(a, o);
-    else orth_product_kernel<S, NMajor, kLast><<<g, S::kThreads, 0, st>>>(a, o);
+    if (step == kNext) orth_product_kernel<S, NMajor, kNext><<<g, S::kThreads, 0, st>>>(a, o, nullptr, 0);
+    else orth_product_kernel<S, NMajor, kLast><<<g, S::kThreads, 0, st>>>(a, o, nullptr, 0);
 }
 
 // The tile whose estimate is least.  Measured (us; 256, 192, 128, 64): 4096 x 4096 bf16, A: 112, 87, 113, 158, the next X:
@@ -322,13 +363,35 @@ void launch_step_parts(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t 
     else if (t256 == least) launch_product<typename TT::T256>(a, o, step, st);
     else launch_product<typename TT::T192>(a, o, step, st);
 }
+template <int NP>
+void launch_shares(TileArgs a, const OrthOut& o, float* sums, hipStream_t st) {
+    typedef typename Tiles<NP>::T64Sym Share;
+    typedef typename Tiles<NP>::T64 Whole;   // the same tiles and wavefronts
+    const int shares = a.splits;
+    orth_share_kernel<Share><<<tile_grid<Share>(a), Share::kThreads, 0, st>>>(a, sums);
+    a.splits = 1;
+    orth_product_kernel<Whole, KMajor, kGram, true><<<tile_grid<Whole>(a), Whole::kThreads, 0, st>>>(a, o, sums, shares);
+}
 void launch_step(const TileArgs& a, const OrthOut& o, OrthStep step, int parts, hipStream_t st) {
     if (parts == 2) launch_step_parts<2>(a, o, step, st);
     else launch_step_parts<1>(a, o, step, st);
 }
 
+// Shares of k of A = X X^T: as many as give every compute unit a tile, where that takes more from the chain of k tiles
+// (0.33 us each) than joining costs, a launch and 16 KB of sums for each (all kernels of a call without and with shares, us:
+// 8 x 66 x 3015 bf16: 339 and 148; 2 x 182 x 1938 fp32: 244, 132; 3 x 500 x 1301: 235, 206; 4 x 128 x 1024: 153, 116; 8 x 300 x 784,
+// 7 tiles less: 192, 184, which its launches take up; 4 x 128 x 512, 6 less: 111, 112).
+constexpr int kShareTiles = 256, kShareGain = 8;
+int shares_of_k(int m, int S, int Lp) {
+    const int side = (S + 63) / 64, kt = Lp / 64;
+    const int64_t tiles = (int64_t)m * side * (side + 1) / 2;
+    const int n = static_cast<int>(std::min<int64_t>(kShareTiles / tiles, kt / 4));
+    return n > 1 && kt - kt / n >= kShareGain ? n : 1;
+}
+
 struct OrthPlan {
-    int S, L, Sp, Lp, parts;     // parts that the products take
+    int S, L, Sp, Lp, parts, shares;   // parts that the products take, shares of A's k
+    float* sums;
     double* norm;
     uint16_t *xp[2], *ap, *bp;   // [2][m][..]
     size_t bytes;
@@ -347,6 +410,8 @@ OrthPlan orth_plan(int m, int rows, int cols, int dtype, void* ws) {
     p.xp[1] = c.take<uint16_t>(nx * 2);
     p.ap = c.take<uint16_t>(na * 2);
     p.bp = c.take<uint16_t>(na * 2);
+    p.shares = shares_of_k(m, p.S, p.Lp);
+    p.sums = c.take<float>(p.shares > 1 ? kShareTiles * 64 * 64 : 0);
     p.bytes = c.used;
     return p;
 }
@@ -385,7 +450,14 @@ int orthogonalise(int m, const OrthIn& in, int dtype, int steps, OrthOut o, cons
         t.a = operand(x, nx, p.Lp, bx, p.S, p.Lp);
         t.b = operand(x, nx, p.Lp, bx, p.S, p.Lp);
         o.to = factors(p.ap, na);
-        launch_step(t, o, kGram, p.parts, st);
+        if (p.shares > 1) {
+            t.splits = p.shares;
+            if (p.parts == 2) launch_shares<2>(t, o, p.sums, st);
+            else launch_shares<1>(t, o, p.sums, st);
+            t.splits = 1;
+        } else {
+            launch_step(t, o, kGram, p.parts, st);
+        }
         t.K = p.Sp;
         t.a = operand(p.ap, na, p.Sp, ba, p.S, p.Sp);
         t.b = operand(p.ap, na, p.Sp, ba, p.S, p.Sp);

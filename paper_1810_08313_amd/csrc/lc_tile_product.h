@@ -300,7 +300,7 @@ struct FetchB<NMajorAny, S> {
 };
 
 struct TilePlace {
-    int batch, tm, tn, split;   // batch < 0: nothing to do
+    int batch, tm, tn, split, tile;   // batch < 0: nothing to do; tile: of the batch
 };
 
 // Tiles of a symmetric result in column tn: those whose first row is not behind the column's last n.
@@ -325,12 +325,13 @@ __device__ __forceinline__ TilePlace tile_place(const TileArgs& a, unsigned bloc
     const int64_t total = (int64_t)a.per_batch * a.batches * a.splits;
     const int64_t chunk = (total + kXcds - 1) / kXcds;
     const int64_t id = (int64_t)(block % kXcds) * chunk + block / kXcds;
-    TilePlace pl{-1, 0, 0, 0};
+    TilePlace pl{-1, 0, 0, 0, 0};
     if (block / kXcds >= chunk || id >= total) return pl;
     const int64_t one = id % ((int64_t)a.per_batch * a.splits);
     pl.batch = (int)(id / ((int64_t)a.per_batch * a.splits));
     pl.split = (int)(one / a.per_batch);
     int t = (int)(one % a.per_batch);
+    pl.tile = t;
     if (a.upper) {
         int tn = 0;
         for (int c; (c = upper_tiles(tn, S::BM, S::BN, a.mt)) <= t; ++tn) t -= c;

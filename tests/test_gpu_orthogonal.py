@@ -282,3 +282,18 @@ def test_bindings_refuse(pkg):
     with pytest.raises(pkg.LcError):
         quad.update_from_grad_orthogonal()
     quad.close()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("m,rows,cols", [(1, 40, 6000), (3, 2500, 100), (2, 130, 900), (1, 450, 3001), (9, 70, 1100)])
+def test_long_sides(pkg, m, rows, cols, bf16):
+    """The first symmetric product in shares of k; no two runs differ."""
+    import torch
+    M = _matrix(m, rows, cols, rows * 7 + cols, "plain").to(torch.bfloat16 if bf16 else torch.float32)
+    out = pkg.orthogonalize(M)
+    again = pkg.orthogonalize(M)
+    torch.cuda.synchronize()
+    assert bool((out == again).all())
+    for i in range(m):
+        want, tol = _reference(M[i], 5, _one_part(M.dtype, rows, cols))
+        _check(f"replica {i}", out[i], want, tol)
