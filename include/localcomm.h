@@ -499,7 +499,8 @@ typedef struct {
     int32_t grad_dtype;         /* of dW and db */
     lc_rows A;                  /* [rows, inputs] */
     lc_rows W;                  /* [inputs, classes], as in a row of X.  bfloat16 is read in place, faster where rows are
-                                 * 16-byte aligned and hold a multiple of 8 classes; fp32 is copied first */
+                                 * 16-byte aligned and hold a multiple of 8 classes; fp32 is read in place where rows
+                                 * are few and weights many, copied first otherwise */
     const float* bias;          /* fp32 [classes] per replica, or NULL */
     int64_t bias_replica;
     const int32_t* labels;      /* device int32 [rows] per replica */

@@ -17,8 +17,8 @@
 // cycle was a conflict.)
 //
 // What bounds it: 64 KB of operands a k tile of 64 come out of the caches at about 10 TB/s over the chip (8192^3, where
-// 8 x 4 tiles of an XCD share them: 0.9 ms alone), LDS reads and the matrix cores could do 0.5 and 0.7 ms: 1.16 ms
-// together, 945 TFLOP/s.  Tiles of 32 k in four buffers: 844.
+// 8 x 4 tiles of an XCD share them: 0.9 ms alone), LDS reads and the matrix cores could do 0.5 and 0.7 ms: 1.08 ms
+// together, 1015 TFLOP/s (n-contiguous B: 988).  Tiles of 32 k in four buffers made 844 where these made 945.
 #pragma once
 #include <type_traits>
 
@@ -47,7 +47,7 @@ __device__ __forceinline__ f32x4 mma32(f16_t, s16x8 a, s16x8 b, f32x4 c) {
 // read: addresses are held inside, and what a lane fetches twice is either not stored (rows of the
 // result) or multiplied with the zeros that stand behind A's k (`len` of B ends before A's).
 struct TileOperand {
-    const uint16_t* p;
+    const uint16_t* p;            // (floats where they are split on the way)
     int64_t row, batch;
     int64_t part[kMaxParts];      // where its parts stand
     int rows, len;                // KMajor: rows of k, `len` of them; NMajor: `rows` k of `len` n.  len % 8 == 0,
