@@ -20,6 +20,8 @@
 //     the result at 64 directions of 512; so: 7e-4, less than bf16 itself).  The result is 1.02 to 1.5 times as far from 64 bits
 //     as its rounding to bf16 alone, 2.0 at the worst (500 x 1301, all singular values alike); smaller matrices would be up
 //     to 2.8 times as far, and their products cost little.
+// Measured: 4096 x 4096 bf16 1.55 ms (B X at 0.95 PFLOP/s; A and A A at 0.75: 253 tiles for 256 compute units), update of
+// 16 x 1024 x 1024 fp32 1.34 ms (B X at 1.05 PFLOP/s of part products), 8 x 300 x 784 fp32 167 us (chains of short launches).
 #include "lc_operators.h"
 #include "lc_tile_product.h"
 
@@ -354,8 +356,8 @@ void launch_step_parts(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t 
     const float least = std::min(std::min(t256, t192), std::min(t128, t64));
     if (t64 == least) {
         tile_grid<typename TT::T64>(a);
-        // not more tiles than compute units: two groups of wavefronts for each half of k and three buffers (768 x 3000 bf16, A:
-        // 25.7 and 18.0 us; 2 x 512 x 2048 fp32: 22.7 and 21.1); more: smaller workgroups, which share a unit (8 x 512 x 1024 fp32: 19 and 25)
+        // not more tiles than compute units: a group of wavefronts for each half of a k tile and three buffers (16 x 300 x 2000
+        // fp32, A: 28.4 and 23.4 us; 3 x 750 x 750 bf16: 10.4 and 9.4); more: smaller workgroups, which share a unit (8 x 512 x 1024 fp32: 19 and 25)
         if (step <= kPoly && (int64_t)a.per_batch * a.batches <= 256) launch_symmetric<typename TT::T64Sym>(a, o, step, st);
         else launch_product<typename TT::T64>(a, o, step, st);
     }
