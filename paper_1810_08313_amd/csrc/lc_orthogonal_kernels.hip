@@ -300,9 +300,9 @@ __global__ void __launch_bounds__(S::kThreads) orth_product_kernel(TileArgs a, O
 
 // Tiles, and what a step costs with them in us, as measured: a tile's start and end, each 64 k of it, how much slower
 // those are with every compute unit busy (the clock falls, and the caches serve all of them), workgroups that share a
-// compute unit, and how much longer a round of all of them takes than one alone.
+// compute unit, how much longer a round of all of them takes than one alone, and what the last step adds to a tile's end.
 struct TileCost {
-    float fixed, per_k, busy, share, together;
+    float fixed, per_k, busy, share, together, last;
 };
 template <int NP>
 struct Tiles {
@@ -311,8 +311,8 @@ struct Tiles {
     typedef TileShape<128, 128, 2, 2, 64, 1, 2> T128;
     typedef TileShape<64, 64, 2, 2, 64, 1, 2> T64;
     typedef TileShape<64, 64, 2, 2, 64, 1, 3, 2> T64Sym;
-    static constexpr TileCost c256{27.f, 1.01f, 0.5f, 1, 1.f}, c192{18.f, 0.70f, 0.5f, 1, 1.f}, c128{12.f, 0.53f, 0.5f, 2, 1.25f},
-        c64{3.3f, 0.45f, 0.15f, 5, 3.1f};
+    static constexpr TileCost c256{27.f, 1.01f, 0.5f, 1, 1.f, 20.f}, c192{18.f, 0.70f, 0.5f, 1, 1.f, 14.f},
+        c128{12.f, 0.53f, 0.5f, 2, 1.25f, 10.f}, c64{3.3f, 0.45f, 0.15f, 5, 2.0f, 2.5f};
 };
 template <>
 struct Tiles<2> {
@@ -321,7 +321,8 @@ struct Tiles<2> {
     typedef TileShape<128, 128, 2, 2, 32, 2, 2> T128;
     typedef TileShape<64, 64, 2, 2, 64, 2, 2> T64;
     typedef TileShape<64, 64, 2, 2, 64, 2, 3, 2> T64Sym;
-    static constexpr TileCost c256{23.5f, 3.17f, 0.5f, 1, 1.f}, c192 = c256, c128{10.3f, 1.58f, 0.5f, 2, 1.25f}, c64{3.2f, 0.60f, 0.15f, 2, 1.42f};
+    static constexpr TileCost c256{23.5f, 3.17f, 0.5f, 1, 1.f, 20.f}, c192 = c256, c128{10.3f, 1.58f, 0.5f, 2, 1.25f, 10.f},
+        c64{3.2f, 0.60f, 0.15f, 2, 1.42f, 2.5f};
 };
 
 template <typename S>
@@ -339,15 +340,16 @@ void launch_product(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t st)
 }
 
 // The tile whose estimate is least.  Measured (us; 256, 192, 128, 64): 4096 x 4096 bf16, A: 112, 87, 113, 158, the next X:
-// 140, 177, 163, 235; 16 x 1024 x 1024 fp32, A: 79, -, 82, 78, the next X: 96, -, 108, 156; 8 x 300 x 784: 56, -, 29, 12
-// and 32, -, 17, 15.  The estimate finds the first or one within 4 %.
+// 140, 177, 163, 235; 16 x 1024 x 1024 fp32, A: 79, -, 82, 78, the next X: 96, -, 108, 156; 4 x 900 x 1800 fp32, A: 114, -, 58,
+// 38, the next X: 78, -, 48, 75; 8 x 512 x 1024 bf16, the next X: 28, -, 15, 13, the last: 52, -, 26, 17; 30 x 400 x 900
+// bf16, the last: 54, -, 54, 44; 12 x 269 x 3703 bf16, the next X: 72, -, 47, 52.  The estimate finds the first or one within 10 %.
 template <int NP>
 void launch_step_parts(TileArgs a, const OrthOut& o, OrthStep step, hipStream_t st) {
     typedef Tiles<NP> TT;
     auto cost = [&](auto shape, const TileCost& c) {
         tile_grid<decltype(shape)>(a);
         const float cus = 256.f, x = static_cast<float>(a.per_batch) * a.batches / cus;   // tiles for each compute unit
-        const float one = c.fixed + c.per_k * (a.K / 64.f) * (1.f + c.busy * std::min(1.f, x));
+        const float one = c.fixed + (step == kLast ? c.last : 0.f) + c.per_k * (a.K / 64.f) * (1.f + c.busy * std::min(1.f, x));
         const float rounds = floorf(x / c.share), rest = x - rounds * c.share;
         return one * (rounds * c.together + (rest <= 0.f ? 0.f : rest <= 1.f ? 1.f : 1.f + (c.together - 1.f) * (rest - 1.f) / (c.share - 1.f)));
     };
