@@ -297,3 +297,29 @@ def test_long_sides(pkg, m, rows, cols, bf16):
     for i in range(m):
         want, tol = _reference(M[i], 5, _one_part(M.dtype, rows, cols))
         _check(f"replica {i}", out[i], want, tol)
+
+
+def test_captured_shares_of_k(pkg):
+    """Replayed with other matrices in place, its workspace shared with nothing else; on two streams at once."""
+    import torch
+    M = _matrix(2, 60, 2500, 9, "plain")
+    pkg.orthogonalize(M)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = pkg.orthogonalize(M)
+    for k in range(3):
+        M.copy_(_matrix(2, 60, 2500, 20 + k, "few"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = pkg.orthogonalize(M)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    Ms = [_matrix(2, 60, 2500, 30 + k, "plain") for k in range(2)]
+    torch.cuda.synchronize()
+    outs = [[pkg.orthogonalize(Ms[k], stream=streams[k]) for _ in range(3)] for k in range(2)]
+    torch.cuda.synchronize()
+    for k in range(2):
+        want = pkg.orthogonalize(Ms[k])
+        assert all(torch.equal(o, want) for o in outs[k])

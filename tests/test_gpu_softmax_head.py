@@ -389,3 +389,25 @@ def test_fp32_weights_split_on_their_way(pkg, rows):
         _check_all(A, W, b, y, loss, row_loss)
         loss, dA, dW, db = pkg.softmax_head_grad(A, Wv, b, y)
         _check_all(A, W, b, y, loss, None, (dA, dW, db))
+
+
+@pytest.mark.parametrize("classes", [1000, 40003])
+def test_captured_fp32_gradients(pkg, classes):
+    """Weights copied in parts and split in place; replays with other inputs."""
+    import torch
+    A, W, b, y = _inputs(3, 40, 72, classes, False, 90, 0.1)
+    pkg.softmax_head_grad(A, W, b, y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = pkg.softmax_head_grad(A, W, b, y)
+    for k in range(3):
+        A2, W2, b2, y2 = _inputs(3, 40, 72, classes, False, 91 + k, 0.3)
+        for to, new in ((A, A2), (W, W2), (b, b2), (y, y2)):
+            to.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = pkg.softmax_head_grad(A, W, b, y)
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
+        _check_all(A, W, b, y, got[0], None, got[1:])
